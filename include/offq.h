@@ -419,6 +419,123 @@ offq_status_t offq_kv_attention_prefill(const uint16_t* q, int64_t B, int64_t T,
                         float sm_scale, int32_t v_hadamard, uint16_t* out, void* stream);
 
 /* ---------------------------------------------------------------------------
+ * The paged 4-bit KV cache: sequences of different lengths in one call, each
+ * in the pages that a table names.  The arithmetic is that of the steps above
+ * (sec. 3.3 step 2(2)/(3), sec. 4.2: one quantizer group per row); the cache is
+ *   k_codes, v_codes  uint8 [num_pages, Hkv, page_size, D/2], 16-byte aligned
+ *   kv_params         int16 [num_pages, Hkv, page_size, 4], 8-byte aligned: the
+ *                     key's scale (fp16 bits) and zero-point, the value's scale
+ *                     and zero-point
+ * with D = head_dim 64 or 128 and page_size a power of two, 16 .. 4096.
+ * Position p of a sequence whose pages are t[0], t[1], ... is the slot
+ * t[p / page_size] * page_size + p % page_size.
+ * ------------------------------------------------------------------------- */
+
+/*
+ * offq_rope_inv_freq -- host helper: the rotary frequencies for
+ * offq_rope_kv_paged (HOST array inv_freq fp32 [rotary_dim / 2]),
+ *     f_i = base^(-2i / rotary_dim),
+ * for a context `factor` >= 1 times the trained one:
+ *   factor = 1          f_i;
+ *   original_len = 0    f_i / factor (every position interpolated);
+ *   original_len > 0    by the turns r_i = original_len * f_i / (2 pi) that a
+ *                       pair makes over the trained context:
+ *                       f_i (k_i + (1 - k_i) / factor), k_i = (r_i - low_turns)
+ *                       / (high_turns - low_turns) clamped to [0, 1]: slow pairs
+ *                       interpolated, fast ones kept.
+ * Computed in fp64, rounded once.  No device is needed.
+ */
+offq_status_t offq_rope_inv_freq(int32_t rotary_dim, double base, double factor, double low_turns,
+                       double high_turns, double original_len, float* inv_freq);
+
+/*
+ * offq_rope_kv_paged -- the new tokens' queries, keys and values from the QKV
+ * projection to attention: per-head RMSNorm, rotary positions, the key's
+ * online Hadamard H3, and the KV4 quantizer writing the pages.  Per token m
+ * and head, in fp32:
+ *     x = x / sqrt(mean_d x_d^2 + eps) * w     (queries, keys; where w is given)
+ *     (x_a, x_b) <- amplitude (x_a cos t - x_b sin t, x_b cos t + x_a sin t),
+ *         t = positions[m] * inv_freq[i], i < rotary_dim / 2, reduced in 64
+ *         bits; (a, b) = (i, i + rotary_dim / 2), or (2i, 2i + 1) where
+ *         interleaved; channels from rotary_dim on stay as they are
+ *     q_out = bf16(x) for queries; for keys and values x (c H x where asked)
+ *         through the quantizer above, one group per head
+ *   qkv        bf16 [M, (Hq + 2 Hkv) D], row stride ldq (a multiple of 8):
+ *              query heads, key heads, value heads; 16-byte aligned.
+ *   q_weight, k_weight  bf16 [D], 16-byte aligned, each NULL for no norm.
+ *   positions  int32 [M]; rotary_dim a multiple of 16, 0 .. D (0: no rotation,
+ *              inv_freq may be NULL); inv_freq fp32 [rotary_dim / 2] (device).
+ *   k_hadamard, v_hadamard  0 or 1: c H on the key / value before it is quantized.
+ *   q_out      bf16 [M, Hq D], row stride ldo (a multiple of 8), 16-byte
+ *              aligned; it may not overlap qkv.
+ *   slots      int64 [M]: where token m's rows go; a slot outside
+ *              [0, num_pages * page_size) writes nothing to the cache.  Two tokens
+ *              of a call with the same slot leave its content unspecified.
+ */
+offq_status_t offq_rope_kv_paged(const uint16_t* qkv, int64_t ldq, int64_t M, int64_t Hq, int64_t Hkv,
+                       int32_t head_dim, const uint16_t* q_weight, const uint16_t* k_weight,
+                       float eps, const int32_t* positions, int32_t rotary_dim,
+                       int32_t interleaved, const float* inv_freq, float amplitude,
+                       int32_t k_hadamard, int32_t v_hadamard, uint16_t* q_out, int64_t ldo,
+                       const int64_t* slots, uint8_t* k_codes, uint8_t* v_codes,
+                       int16_t* kv_params, int64_t num_pages, int32_t page_size, void* stream);
+
+/*
+ * offq_kv_dequantize_paged -- cached rows back as bf16 values:
+ *     k_out[m, h] = bf16(s (c - z)), or bf16(c H (s (c - z))) with k_hadamard
+ *     (the rotation undone); v_out likewise.
+ *   slots      int64 [M], in any order, repeats allowed; rows of a slot outside
+ *              [0, num_pages * page_size) are left as they were.
+ *   k_out, v_out  bf16 [M, Hkv D], row strides ldk, ldv (multiples of 8),
+ *              16-byte aligned; either may be NULL (not both).
+ */
+offq_status_t offq_kv_dequantize_paged(const uint8_t* k_codes, const uint8_t* v_codes,
+                             const int16_t* kv_params, int64_t num_pages, int32_t page_size,
+                             int64_t Hkv, int32_t head_dim, const int64_t* slots, int64_t M,
+                             int32_t k_hadamard, int32_t v_hadamard, uint16_t* k_out, int64_t ldk,
+                             uint16_t* v_out, int64_t ldv, void* stream);
+
+/*
+ * offq_kv_attention_paged -- causal attention of the new tokens of B sequences,
+ * packed one after the other, over the paged cache (which holds their own rows
+ * already): single tokens, drafted tokens, chunks of a prompt and whole prompts,
+ * mixed freely.  Sequence b has the n = q_starts[b + 1] - q_starts[b] query rows
+ * from q_starts[b] on and seq_lens[b] positions; its query i sits at position
+ * seq_lens[b] - n + i and sees the positions up to its own:
+ *     q_r = c H q with k_hadamard, else q
+ *     s_j = sm_scale sk_j sum_d q_r[d] (ck_j[d] - zk_j),  p = softmax(s)
+ *     out = bf16(sum_j p_j sv_j (cv_j - zv_j)), c H of that sum with v_hadamard
+ *   q          bf16 [M, Hq D], row stride ldq (a multiple of 8), 16-byte aligned;
+ *              query head h reads key/value head h / (Hq / Hkv).
+ *   q_starts   int32 [B + 1] (device), ascending, within [0, M]; seq_lens int32 [B]
+ *              (device).  Rows in no sequence are left as they were.
+ *   max_new    the most new tokens of a sequence (rows of a sequence past its
+ *              first max_new are left as they were).
+ *   page_table int32 [B, max_pages] (device): a sequence's pages in order.  A
+ *              position whose page is outside [0, num_pages), or past the table,
+ *              is not seen; a row that sees no position gives 0.
+ *   out        bf16 [M, Hq D], row stride ldo (a multiple of 8), 16-byte aligned;
+ *              it may not overlap q.
+ *   workspace  caller-owned device buffer of at least
+ *              offq_kv_attention_paged_workspace_bytes(M, B, Hq, Hkv, head_dim,
+ *              max_new) bytes, 16-byte aligned (NULL where that is 0); scratch.
+ *              Calls that share a workspace must be ordered on one stream.
+ * Lengths and tables are read on the device only, so that a captured call
+ * replays with new ones.
+ */
+offq_status_t offq_kv_attention_paged(const uint16_t* q, int64_t ldq, int64_t M, int64_t Hq, int64_t Hkv,
+                            int32_t head_dim, const int32_t* q_starts, const int32_t* seq_lens,
+                            int64_t B, int64_t max_new, const int32_t* page_table,
+                            int64_t max_pages, const uint8_t* k_codes, const uint8_t* v_codes,
+                            const int16_t* kv_params, int64_t num_pages, int32_t page_size,
+                            float sm_scale, int32_t k_hadamard, int32_t v_hadamard, uint16_t* out,
+                            int64_t ldo, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Bytes of workspace offq_kv_attention_paged needs; 0 also for invalid sizes. */
+int64_t offq_kv_attention_paged_workspace_bytes(int64_t M, int64_t B, int64_t Hq, int64_t Hkv,
+                                                int32_t head_dim, int64_t max_new);
+
+/* ---------------------------------------------------------------------------
  * Offline calibration (sec. 3.1 top-1 PCA, sec. 3.2 group-wise offsetting,
  * sec. 3.3 steps 1-2): from calibration activations to the fused, permuted
  * and rotated fp32 weights that offq_pack_weights then quantizes.  These run

@@ -16,6 +16,14 @@ arguments.  Entry points (same names as ``include/offq.h``):
     offq_rope_kv_prefill(qkv, B, Hq, Hkv, positions, cache, rope_base=500000.0, ...)
     offq_kv_attention_prefill(q, cache, past, sm_scale=None, v_hadamard=False, out=None)
 
+The paged 4-bit cache, sequences of different lengths in one call:
+
+    paged_cache(num_pages, Hkv, page_size, head_dim=128)
+    offq_rope_inv_freq(rotary_dim, base=500000.0, factor=1.0, ...)
+    offq_rope_kv_paged(qkv, Hq, positions, slots, cache, inv_freq, ...)
+    offq_kv_attention_paged(q, q_starts, seq_lens, page_table, cache, max_new, ...)
+    offq_kv_dequantize_paged(cache, slots, k_hadamard=True, v_hadamard=False)
+
 Offline calibration: offq_top1_select, offq_channel_absmax, offq_gram, offq_eigh,
 offq_group_permutation, offq_build_rotation, offq_fuse_weights, offq_permute_rows.
 
@@ -43,6 +51,12 @@ _EXPORTS = frozenset((
     "offq_rope_kv_append",
     "offq_rope_kv_prefill",
     "offq_kv_attention_prefill",
+    "paged_cache",
+    "offq_rope_inv_freq",
+    "offq_rope_kv_paged",
+    "offq_kv_dequantize_paged",
+    "offq_kv_attention_paged",
+    "offq_kv_attention_paged_workspace_bytes",
     "offq_swiglu",
     "offq_kv_attention_decode",
     "offq_kv_attention_decode_quantize",

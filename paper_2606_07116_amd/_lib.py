@@ -41,6 +41,11 @@ EXPORTED = (
     "offq_kv_attention_prefill",
     "offq_add_rmsnorm_quantize",
     "offq_swiglu_rotate_quantize",
+    "offq_rope_inv_freq",
+    "offq_rope_kv_paged",
+    "offq_kv_dequantize_paged",
+    "offq_kv_attention_paged",
+    "offq_kv_attention_paged_workspace_bytes",
     "offq_top1_workspace_bytes",
     "offq_top1_select",
     "offq_channel_absmax",
@@ -122,6 +127,16 @@ def _load():
         "offq_kv_attention_decode_noalloc": (ctypes.c_int, [vp, vp, vp, vp, vp, vp, vp, i64, i64, i64,
                                                             i64, i64, i32, ctypes.c_float, i32, vp,
                                                             vp]),
+        "offq_rope_inv_freq": (ctypes.c_int, [i32, f64, f64, f64, f64, f64, vp]),
+        "offq_rope_kv_paged": (ctypes.c_int, [vp, i64, i64, i64, i64, i32, vp, vp, ctypes.c_float,
+                                              vp, i32, i32, vp, ctypes.c_float, i32, i32, vp, i64,
+                                              vp, vp, vp, vp, i64, i32, vp]),
+        "offq_kv_dequantize_paged": (ctypes.c_int, [vp, vp, vp, i64, i32, i64, i32, vp, i64, i32,
+                                                    i32, vp, i64, vp, i64, vp]),
+        "offq_kv_attention_paged": (ctypes.c_int, [vp, i64, i64, i64, i64, i32, vp, vp, i64, i64,
+                                                   vp, i64, vp, vp, vp, i64, i32, ctypes.c_float,
+                                                   i32, i32, vp, i64, vp, i64, vp]),
+        "offq_kv_attention_paged_workspace_bytes": (i64, [i64, i64, i64, i64, i32, i64]),
         "offq_top1_workspace_bytes": (i64, [i64, i64]),
         "offq_top1_select": (ctypes.c_int, [vp, i64, i64, i64, i64, i64, vp, vp, i64, vp, i64, vp]),
         "offq_channel_absmax": (ctypes.c_int, [vp, i64, i64, i64, vp, vp]),
@@ -304,6 +319,42 @@ def offq_kv_attention_prefill_raw(q, B, T, Hq, Hkv, head_dim, past, k_codes, k_s
     return lib.offq_kv_attention_prefill(q, B, T, Hq, Hkv, head_dim, past, k_codes, k_scale,
                                          k_zero, v_codes, v_scale, v_zero, s_cap, sm_scale,
                                          v_hadamard, out, stream)
+
+
+def offq_rope_inv_freq_raw(rotary_dim, base, factor, low_turns, high_turns, original_len, inv_freq):
+    return lib.offq_rope_inv_freq(rotary_dim, base, factor, low_turns, high_turns, original_len,
+                                  inv_freq)
+
+
+def offq_rope_kv_paged_raw(qkv, ldq, M, Hq, Hkv, head_dim, q_weight, k_weight, eps, positions,
+                           rotary_dim, interleaved, inv_freq, amplitude, k_hadamard, v_hadamard,
+                           q_out, ldo, slots, k_codes, v_codes, kv_params, num_pages, page_size,
+                           stream):
+    return lib.offq_rope_kv_paged(qkv, ldq, M, Hq, Hkv, head_dim, q_weight, k_weight, eps,
+                                  positions, rotary_dim, interleaved, inv_freq, amplitude,
+                                  k_hadamard, v_hadamard, q_out, ldo, slots, k_codes, v_codes,
+                                  kv_params, num_pages, page_size, stream)
+
+
+def offq_kv_dequantize_paged_raw(k_codes, v_codes, kv_params, num_pages, page_size, Hkv, head_dim,
+                                 slots, M, k_hadamard, v_hadamard, k_out, ldk, v_out, ldv, stream):
+    return lib.offq_kv_dequantize_paged(k_codes, v_codes, kv_params, num_pages, page_size, Hkv,
+                                        head_dim, slots, M, k_hadamard, v_hadamard, k_out, ldk,
+                                        v_out, ldv, stream)
+
+
+def offq_kv_attention_paged_raw(q, ldq, M, Hq, Hkv, head_dim, q_starts, seq_lens, B, max_new,
+                                page_table, max_pages, k_codes, v_codes, kv_params, num_pages,
+                                page_size, sm_scale, k_hadamard, v_hadamard, out, ldo, workspace,
+                                workspace_bytes, stream):
+    return lib.offq_kv_attention_paged(q, ldq, M, Hq, Hkv, head_dim, q_starts, seq_lens, B, max_new,
+                                       page_table, max_pages, k_codes, v_codes, kv_params,
+                                       num_pages, page_size, sm_scale, k_hadamard, v_hadamard, out,
+                                       ldo, workspace, workspace_bytes, stream)
+
+
+def offq_kv_attention_paged_workspace_bytes(M, B, Hq, Hkv, head_dim, max_new):
+    return lib.offq_kv_attention_paged_workspace_bytes(M, B, Hq, Hkv, head_dim, max_new)
 
 
 # ------------------------------------------------------------ tensor wrappers
@@ -693,6 +744,172 @@ def offq_kv_attention_prefill(q, cache, past, sm_scale=None, v_hadamard=False, o
                                          _ptr(cache["v_scale"]), _ptr(cache["v_zero"]), s_cap,
                                          float(sm_scale), int(bool(v_hadamard)), _ptr(out),
                                          _stream()), "offq_kv_attention_prefill")
+    return out
+
+
+# ----------------------------------------------------------- paged 4-bit cache
+def paged_cache(num_pages, Hkv, page_size, head_dim=128, device="cuda"):
+    """The arrays of a paged 4-bit cache, zeroed: k_codes, v_codes u8 [num_pages, Hkv,
+    page_size, head_dim/2], kv_params int16 [num_pages, Hkv, page_size, 4] (key scale as fp16
+    bits, key zero-point, value scale, value zero-point)."""
+    torch = _torch()
+    shape = (num_pages, Hkv, page_size)
+    return {"k_codes": torch.zeros(shape + (head_dim // 2,), dtype=torch.uint8, device=device),
+            "v_codes": torch.zeros(shape + (head_dim // 2,), dtype=torch.uint8, device=device),
+            "kv_params": torch.zeros(shape + (4,), dtype=torch.int16, device=device)}
+
+
+def _paged_operands(cache, device):
+    """(pointers, num_pages, page_size, Hkv, head_dim) of a paged cache on `device`."""
+    torch = _torch()
+    kc, vc, par = cache["k_codes"], cache["v_codes"], cache["kv_params"]
+    for t, dt, n in ((kc, torch.uint8, "k_codes"), (vc, torch.uint8, "v_codes"),
+                     (par, torch.int16, "kv_params")):
+        _need(t, dt, n, 4)
+        if not t.is_contiguous():
+            raise ValueError(f"{n} must be contiguous")
+        _same_device(t, device, n)
+    pages, Hkv, page_size, half = kc.shape
+    if vc.shape != kc.shape or par.shape != (pages, Hkv, page_size, 4):
+        raise ValueError("the cache arrays' shapes do not match")
+    return (_ptr(kc), _ptr(vc), _ptr(par)), pages, page_size, Hkv, 2 * half
+
+
+def _same_device(t, device, name):
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+
+
+def _index(t, dtype, shape, device, name):
+    _need(t, dtype, name, len(shape))
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {list(shape)} tensor")
+    _same_device(t, device, name)
+
+
+def _heads(t, name, device, M=None, H=None, D=None):
+    """Row stride of a bf16 [M, H, D] tensor whose rows [H, D] are contiguous."""
+    _need(t, _torch().bfloat16, name, 3)
+    if (M is not None and t.shape[0] != M) or (H is not None and t.shape[1] != H) \
+            or (D is not None and t.shape[2] != D):
+        raise ValueError(f"{name} must be [{M}, {H}, {D}], got {list(t.shape)}")
+    if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+        raise ValueError(f"{name} must have contiguous rows")
+    _same_device(t, device, name)
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def offq_rope_inv_freq(rotary_dim, base=500000.0, factor=1.0, low_turns=1.0, high_turns=4.0,
+                       original_len=0, device="cuda"):
+    """Rotary frequencies fp32 [rotary_dim / 2] on `device`: plain (factor 1), every position
+    interpolated (original_len 0), or by the turns a pair makes over original_len positions."""
+    torch = _torch()
+    out = torch.empty((max(int(rotary_dim), 0) // 2,), dtype=torch.float32)
+    _check(lib.offq_rope_inv_freq(int(rotary_dim), float(base), float(factor), float(low_turns),
+                                  float(high_turns), float(original_len), _ptr(out)),
+           "offq_rope_inv_freq")
+    return out.to(device)
+
+
+def offq_rope_kv_paged(qkv, Hq, positions, slots, cache, inv_freq=None, interleaved=False,
+                       amplitude=1.0, q_weight=None, k_weight=None, eps=1e-6, k_hadamard=True,
+                       v_hadamard=False, out=None):
+    """Norm (where a weight is given), rotary positions, H3 and the 4-bit page write of the rows
+    of a QKV projection.
+
+    qkv: bf16 [M, (Hq + 2 Hkv) * D]; positions int32 [M]; slots int64 [M] (page * page_size +
+    offset; outside the cache: not written); cache: see paged_cache; inv_freq fp32
+    [rotary_dim / 2] (None: no rotation); weights bf16 [D].  Returns q bf16 [M, Hq, D]."""
+    torch = _torch()
+    _need(qkv, torch.bfloat16, "qkv", 2)
+    dev = qkv.device
+    ptrs, pages, page_size, Hkv, D = _paged_operands(cache, dev)
+    M = qkv.shape[0]
+    if qkv.shape[1] != (Hq + 2 * Hkv) * D:
+        raise ValueError("qkv must have (Hq + 2 Hkv) * head_dim columns")
+    ldq = _rows(qkv, "qkv") if M > 1 else qkv.shape[1]
+    _index(positions, torch.int32, (M,), dev, "positions")
+    _index(slots, torch.int64, (M,), dev, "slots")
+    rotary = 0
+    if inv_freq is not None:
+        rotary = 2 * inv_freq.numel()
+        _index(inv_freq, torch.float32, (rotary // 2,), dev, "inv_freq")
+    for w, n in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if w is not None:
+            _index(w, torch.bfloat16, (D,), dev, n)
+    if out is None:
+        out = torch.empty((M, Hq, D), dtype=torch.bfloat16, device=dev)
+    ldo = _heads(out, "out", dev, M, Hq, D)
+    with torch.cuda.device(dev):
+        _check(lib.offq_rope_kv_paged(_ptr(qkv), ldq, M, Hq, Hkv, D, _ptr(q_weight), _ptr(k_weight),
+                                      float(eps), _ptr(positions), rotary, int(bool(interleaved)),
+                                      _ptr(inv_freq), float(amplitude), int(bool(k_hadamard)),
+                                      int(bool(v_hadamard)), _ptr(out), ldo, _ptr(slots), *ptrs,
+                                      pages, page_size, _stream()), "offq_rope_kv_paged")
+    return out
+
+
+def offq_kv_dequantize_paged(cache, slots, k_hadamard=True, v_hadamard=False, k_out=None,
+                             v_out=None):
+    """The cached rows at `slots` (int64 [M], any order) as bf16 (k, v), each [M, Hkv, D], the
+    rotations undone where asked.  Rows of a slot outside the cache are left as they were
+    (zero in new outputs)."""
+    torch = _torch()
+    _need(slots, torch.int64, "slots", 1)
+    dev = slots.device
+    ptrs, pages, page_size, Hkv, D = _paged_operands(cache, dev)
+    M = slots.shape[0]
+    _index(slots, torch.int64, (M,), dev, "slots")
+    k_out, v_out = (torch.zeros((M, Hkv, D), dtype=torch.bfloat16, device=dev) if t is None else t
+                    for t in (k_out, v_out))
+    ldk, ldv = _heads(k_out, "k_out", dev, M, Hkv, D), _heads(v_out, "v_out", dev, M, Hkv, D)
+    with torch.cuda.device(dev):
+        _check(lib.offq_kv_dequantize_paged(*ptrs, pages, page_size, Hkv, D, _ptr(slots), M,
+                                            int(bool(k_hadamard)), int(bool(v_hadamard)),
+                                            _ptr(k_out), ldk, _ptr(v_out), ldv, _stream()),
+               "offq_kv_dequantize_paged")
+    return k_out, v_out
+
+
+def offq_kv_attention_paged(q, q_starts, seq_lens, page_table, cache, max_new, sm_scale=None,
+                            k_hadamard=True, v_hadamard=False, out=None, workspace=None):
+    """Causal attention of packed new tokens over a paged 4-bit cache.
+
+    q: bf16 [M, Hq, D]; q_starts int32 [B + 1] and seq_lens int32 [B]: sequence b's rows
+    q_starts[b] .. q_starts[b + 1] - 1 are its last positions of seq_lens[b]; page_table int32
+    [B, max_pages] (entries outside the cache: positions not seen); max_new: the most new tokens
+    of a sequence.  sm_scale defaults to 1/sqrt(D).  Returns out bf16 [M, Hq, D] (rows in no
+    sequence are not written)."""
+    torch = _torch()
+    _need(q, torch.bfloat16, "q", 3)
+    dev = q.device
+    ptrs, pages, page_size, Hkv, D = _paged_operands(cache, dev)
+    M, Hq = q.shape[:2]
+    ldq = _heads(q, "q", dev, M, Hq, D)
+    _need(seq_lens, torch.int32, "seq_lens", 1)
+    B = seq_lens.shape[0]
+    _index(seq_lens, torch.int32, (B,), dev, "seq_lens")
+    _index(q_starts, torch.int32, (B + 1,), dev, "q_starts")
+    _need(page_table, torch.int32, "page_table", 2)
+    _index(page_table, torch.int32, (B, page_table.shape[1]), dev, "page_table")
+    if out is None:
+        out = torch.empty((M, Hq, D), dtype=torch.bfloat16, device=dev)
+    ldo = _heads(out, "out", dev, M, Hq, D)
+    need = lib.offq_kv_attention_paged_workspace_bytes(M, B, Hq, Hkv, D, int(max_new))
+    if workspace is None and need:
+        workspace = torch.empty((need,), dtype=torch.uint8, device=dev)
+    if workspace is not None:
+        _need(workspace, torch.uint8, "workspace", 1)
+        _same_device(workspace, dev, "workspace")
+    if sm_scale is None:
+        sm_scale = 1.0 / float(D) ** 0.5
+    with torch.cuda.device(dev):
+        _check(lib.offq_kv_attention_paged(
+            _ptr(q), ldq, M, Hq, Hkv, D, _ptr(q_starts), _ptr(seq_lens), B, int(max_new),
+            _ptr(page_table), page_table.shape[1], *ptrs, pages, page_size, float(sm_scale),
+            int(bool(k_hadamard)), int(bool(v_hadamard)), _ptr(out), ldo, _ptr(workspace),
+            workspace.numel() if workspace is not None else 0, _stream()),
+            "offq_kv_attention_paged")
     return out
 
 

@@ -127,6 +127,47 @@ hipError_t launch_rope_kv_append(const uint16_t* qkv, int64_t ldq, int64_t M, in
                                  int16_t* vz, int64_t s_cap, float* k_dbg, float* v_dbg,
                                  hipStream_t stream);
 
+// The paged 4-bit cache (paged.h; paged_cache.hip, paged_attention.hip).
+struct PagedCache;
+struct RopeKvPagedArgs {
+  const uint16_t* qkv;
+  int64_t ldq, M;
+  int Hq;
+  const uint16_t *q_weight, *k_weight;
+  float eps;
+  const int32_t* positions;
+  int rotary, pairs;
+  const float* inv_freq;
+  float amplitude;
+  int k_had, v_had;
+  uint16_t* q_out;
+  int64_t ldo;
+  const int64_t* slots;
+};
+hipError_t launch_rope_kv_paged(const RopeKvPagedArgs& a, const PagedCache& c, int head_dim,
+                                hipStream_t stream);
+hipError_t launch_kv_dequantize_paged(const PagedCache& c, int head_dim, const int64_t* slots,
+                                      int64_t M, bool k_had, bool v_had, uint16_t* k_out,
+                                      int64_t ldk, uint16_t* v_out, int64_t ldv,
+                                      hipStream_t stream);
+struct PagedAttentionArgs {
+  const uint16_t* q;
+  int64_t ldq;
+  int M, Hq;
+  const int32_t *q_starts, *seq_lens;
+  int B, max_new;
+  const int32_t* page_table;
+  int max_pages;
+  float sm_scale;
+  int k_had, v_had;
+  uint16_t* out;
+  int64_t ldo;
+};
+int64_t kv_attention_paged_workspace_floats(int64_t M, int64_t B, int64_t Hq, int64_t Hkv,
+                                            int head_dim, int64_t max_new);
+hipError_t launch_kv_attention_paged(const PagedAttentionArgs& a, const PagedCache& c, int head_dim,
+                                     float* workspace, hipStream_t stream);
+
 // offline calibration (calibration.hip)
 hipError_t launch_top1_select(const uint16_t* x, int64_t n_seq, int64_t L, int64_t D,
                               int64_t ld_tok, int64_t ld_seq, int32_t* idx, float* X, int64_t ldX,

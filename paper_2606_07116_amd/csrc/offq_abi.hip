@@ -8,6 +8,7 @@
 #include "../../include/offq.h"
 #include "common.h"
 #include "internal.h"
+#include "paged.h"
 
 namespace {
 
@@ -431,6 +432,211 @@ offq_status_t offq_kv_attention_prefill(const uint16_t* q, int64_t B, int64_t T,
                                                     sm_scale, v_hadamard != 0, out,
                                                     (hipStream_t)stream),
                   "kv_attention_prefill");
+}
+
+namespace {
+// The parts of the paged cache that every entry point checks alike.
+offq_status_t check_paged(int64_t Hkv, int32_t head_dim, int64_t num_pages, int32_t page_size,
+                          int32_t k_hadamard, int32_t v_hadamard) {
+  if (Hkv <= 0 || num_pages <= 0) return fail(OFFQ_ERR_INVALID, "need Hkv, num_pages > 0");
+  if (head_dim != 64 && head_dim != 128)
+    return fail(OFFQ_ERR_UNSUPPORTED, "head_dim = %d (64 or 128)", head_dim);
+  const int lp = ilog2_pow2(page_size);
+  if (lp < 0) return fail(OFFQ_ERR_INVALID, "page_size = %d is not a power of two", page_size);
+  if (lp < 4 || lp > 12)
+    return fail(OFFQ_ERR_UNSUPPORTED, "page_size = %d outside [16, 4096]", page_size);
+  if ((k_hadamard != 0 && k_hadamard != 1) || (v_hadamard != 0 && v_hadamard != 1))
+    return fail(OFFQ_ERR_INVALID, "k_hadamard / v_hadamard must be 0 or 1");
+  if (Hkv > (1 << 16) || num_pages > (int64_t(1) << 40) / (Hkv * page_size))
+    return fail(OFFQ_ERR_UNSUPPORTED, "sizes too large");
+  return OFFQ_OK;
+}
+
+offq_status_t check_paged_pointers(const uint8_t* k_codes, const uint8_t* v_codes,
+                                   const int16_t* kv_params) {
+  if (!k_codes || !v_codes || !kv_params) return fail(OFFQ_ERR_INVALID, "null pointer argument");
+  if (!aligned(k_codes, 16) || !aligned(v_codes, 16) || !aligned(kv_params, 8))
+    return fail(OFFQ_ERR_INVALID, "misaligned pointer (codes: 16 B; kv_params: 8 B)");
+  return OFFQ_OK;
+}
+
+// [a, a + na) and [b, b + nb) share a byte
+bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
+}
+}  // namespace
+
+offq_status_t offq_rope_inv_freq(int32_t rotary_dim, double base, double factor, double low_turns,
+                       double high_turns, double original_len, float* inv_freq) {
+  if (rotary_dim <= 0 || rotary_dim % 2)
+    return fail(OFFQ_ERR_INVALID, "rotary_dim must be positive and even");
+  if (!(base > 1.0) || base > 1e30) return fail(OFFQ_ERR_INVALID, "base must be > 1");
+  if (!(factor >= 1.0) || factor > 1e9) return fail(OFFQ_ERR_INVALID, "factor must be >= 1");
+  if (!(original_len >= 0.0) || original_len > 1e12)
+    return fail(OFFQ_ERR_INVALID, "original_len must be >= 0");
+  if (original_len > 0.0 && !(low_turns >= 0.0 && high_turns > low_turns && high_turns <= 1e12))
+    return fail(OFFQ_ERR_INVALID, "need 0 <= low_turns < high_turns");
+  if (!inv_freq) return fail(OFFQ_ERR_INVALID, "null pointer argument");
+  for (int i = 0; i < rotary_dim / 2; ++i) {
+    const double f = __builtin_pow(base, -2.0 * i / rotary_dim);
+    double keep = 0.0;
+    if (original_len > 0.0) {
+      const double turns = original_len * f / 6.283185307179586;
+      keep = (turns - low_turns) / (high_turns - low_turns);
+      keep = keep < 0.0 ? 0.0 : keep > 1.0 ? 1.0 : keep;
+    }
+    inv_freq[i] = (float)(f * (keep + (1.0 - keep) / factor));
+  }
+  return ok();
+}
+
+offq_status_t offq_rope_kv_paged(const uint16_t* qkv, int64_t ldq, int64_t M, int64_t Hq, int64_t Hkv,
+                       int32_t head_dim, const uint16_t* q_weight, const uint16_t* k_weight,
+                       float eps, const int32_t* positions, int32_t rotary_dim,
+                       int32_t interleaved, const float* inv_freq, float amplitude,
+                       int32_t k_hadamard, int32_t v_hadamard, uint16_t* q_out, int64_t ldo,
+                       const int64_t* slots, uint8_t* k_codes, uint8_t* v_codes,
+                       int16_t* kv_params, int64_t num_pages, int32_t page_size, void* stream) {
+  if (M < 0 || Hq <= 0) return fail(OFFQ_ERR_INVALID, "need M >= 0, Hq > 0");
+  if (offq_status_t st = check_paged(Hkv, head_dim, num_pages, page_size, k_hadamard, v_hadamard))
+    return st;
+  if (Hq > (1 << 16) || M > (int64_t(1) << 31) - 1 || ldq > (int64_t(1) << 40) ||
+      ldo > (int64_t(1) << 40))
+    return fail(OFFQ_ERR_UNSUPPORTED, "sizes too large");
+  if (ldq < (Hq + 2 * Hkv) * head_dim || ldq % 8 || ldo < Hq * head_dim || ldo % 8)
+    return fail(OFFQ_ERR_INVALID,
+                "need ldq >= (Hq + 2 Hkv) head_dim, ldo >= Hq head_dim, both multiples of 8");
+  if (rotary_dim < 0 || rotary_dim > head_dim || rotary_dim % 16)
+    return fail(OFFQ_ERR_INVALID, "rotary_dim must be a multiple of 16 in [0, head_dim]");
+  if (interleaved != 0 && interleaved != 1)
+    return fail(OFFQ_ERR_INVALID, "interleaved must be 0 or 1");
+  if (!(eps >= 0.0f) || eps > 1e30f) return fail(OFFQ_ERR_INVALID, "eps must be finite and >= 0");
+  if (!(__builtin_fabsf(amplitude) <= 1e30f))
+    return fail(OFFQ_ERR_INVALID, "amplitude must be finite");
+  if (M == 0) return ok();  // empty: pointers may be NULL
+  if (!qkv || !positions || !q_out || !slots || (rotary_dim && !inv_freq))
+    return fail(OFFQ_ERR_INVALID, "null pointer argument");
+  if (offq_status_t st = check_paged_pointers(k_codes, v_codes, kv_params)) return st;
+  if (!aligned(qkv, 16) || !aligned(q_out, 16) || !aligned(q_weight, 16) ||
+      !aligned(k_weight, 16) || !aligned(positions, 4) || !aligned(inv_freq, 4) ||
+      !aligned(slots, 8))
+    return fail(OFFQ_ERR_INVALID, "misaligned pointer (qkv, q_out, weights: 16 B; slots: 8 B)");
+  if (overlap(qkv, 2 * ((M - 1) * ldq + (Hq + 2 * Hkv) * head_dim), q_out,
+              2 * ((M - 1) * ldo + Hq * head_dim)))
+    return fail(OFFQ_ERR_INVALID, "q_out overlaps qkv");
+  if (offq_status_t st = check_device()) return st;
+  const offq::PagedCache c = {k_codes, v_codes, kv_params, num_pages, ilog2_pow2(page_size),
+                              (int)Hkv};
+  const offq::RopeKvPagedArgs a = {qkv,        ldq,        M,           (int)Hq,    q_weight,
+                                   k_weight,   eps,        positions,   rotary_dim, interleaved,
+                                   inv_freq,   amplitude,  k_hadamard,  v_hadamard, q_out,
+                                   ldo,        slots};
+  return launched(offq::launch_rope_kv_paged(a, c, head_dim, (hipStream_t)stream), "rope_kv_paged");
+}
+
+offq_status_t offq_kv_dequantize_paged(const uint8_t* k_codes, const uint8_t* v_codes,
+                             const int16_t* kv_params, int64_t num_pages, int32_t page_size,
+                             int64_t Hkv, int32_t head_dim, const int64_t* slots, int64_t M,
+                             int32_t k_hadamard, int32_t v_hadamard, uint16_t* k_out, int64_t ldk,
+                             uint16_t* v_out, int64_t ldv, void* stream) {
+  if (M < 0) return fail(OFFQ_ERR_INVALID, "need M >= 0");
+  if (offq_status_t st = check_paged(Hkv, head_dim, num_pages, page_size, k_hadamard, v_hadamard))
+    return st;
+  if (M > (int64_t(1) << 31) - 1 || M * Hkv > (int64_t(1) << 34) || ldk > (int64_t(1) << 40) ||
+      ldv > (int64_t(1) << 40))
+    return fail(OFFQ_ERR_UNSUPPORTED, "sizes too large");
+  if ((k_out && (ldk < Hkv * head_dim || ldk % 8)) || (v_out && (ldv < Hkv * head_dim || ldv % 8)))
+    return fail(OFFQ_ERR_INVALID, "need ldk, ldv >= Hkv head_dim, multiples of 8");
+  if (M == 0) return ok();  // empty: pointers may be NULL
+  if (!slots || (!k_out && !v_out)) return fail(OFFQ_ERR_INVALID, "null pointer argument");
+  if (offq_status_t st = check_paged_pointers(k_codes, v_codes, kv_params)) return st;
+  if (!aligned(slots, 8) || !aligned(k_out, 16) || !aligned(v_out, 16))
+    return fail(OFFQ_ERR_INVALID, "misaligned pointer (k_out, v_out: 16 B; slots: 8 B)");
+  if (k_out && v_out &&
+      overlap(k_out, 2 * ((M - 1) * ldk + Hkv * head_dim), v_out,
+              2 * ((M - 1) * ldv + Hkv * head_dim)) &&
+      !(ldk == ldv && ldk >= 2 * Hkv * head_dim &&
+        (k_out + Hkv * head_dim <= v_out ? v_out + Hkv * head_dim <= k_out + ldk
+                                         : v_out + Hkv * head_dim <= k_out &&
+                                               k_out + Hkv * head_dim <= v_out + ldv)))
+    return fail(OFFQ_ERR_INVALID, "k_out overlaps v_out");
+  if (offq_status_t st = check_device()) return st;
+  // the kernel only reads the cache
+  const offq::PagedCache c = {const_cast<uint8_t*>(k_codes), const_cast<uint8_t*>(v_codes),
+                              const_cast<int16_t*>(kv_params), num_pages, ilog2_pow2(page_size),
+                              (int)Hkv};
+  return launched(offq::launch_kv_dequantize_paged(c, head_dim, slots, M, k_hadamard != 0,
+                                                   v_hadamard != 0, k_out, ldk, v_out, ldv,
+                                                   (hipStream_t)stream),
+                  "kv_dequantize_paged");
+}
+
+namespace {
+bool paged_attention_sizes(int64_t M, int64_t B, int64_t Hq, int64_t Hkv, int32_t head_dim,
+                           int64_t max_new) {
+  return M >= 0 && B >= 0 && max_new >= 0 && Hq > 0 && Hkv > 0 && Hq % Hkv == 0 &&
+         (head_dim == 64 || head_dim == 128) && M <= (1 << 24) && B <= (1 << 20) &&
+         Hq <= (1 << 12) && M * Hq <= (int64_t(1) << 31) && B * Hkv <= (1 << 22);
+}
+}  // namespace
+
+int64_t offq_kv_attention_paged_workspace_bytes(int64_t M, int64_t B, int64_t Hq, int64_t Hkv,
+                                                int32_t head_dim, int64_t max_new) {
+  if (!paged_attention_sizes(M, B, Hq, Hkv, head_dim, max_new) || !M || !B || !max_new) return 0;
+  return offq::kv_attention_paged_workspace_floats(M, B, Hq, Hkv, head_dim,
+                                                   max_new < M ? max_new : M) *
+         (int64_t)sizeof(float);
+}
+
+offq_status_t offq_kv_attention_paged(const uint16_t* q, int64_t ldq, int64_t M, int64_t Hq, int64_t Hkv,
+                            int32_t head_dim, const int32_t* q_starts, const int32_t* seq_lens,
+                            int64_t B, int64_t max_new, const int32_t* page_table,
+                            int64_t max_pages, const uint8_t* k_codes, const uint8_t* v_codes,
+                            const int16_t* kv_params, int64_t num_pages, int32_t page_size,
+                            float sm_scale, int32_t k_hadamard, int32_t v_hadamard, uint16_t* out,
+                            int64_t ldo, void* workspace, int64_t workspace_bytes, void* stream) {
+  if (M < 0 || B < 0 || max_new < 0 || Hq <= 0 || max_pages <= 0)
+    return fail(OFFQ_ERR_INVALID, "need M, B, max_new >= 0 and Hq, max_pages > 0");
+  if (offq_status_t st = check_paged(Hkv, head_dim, num_pages, page_size, k_hadamard, v_hadamard))
+    return st;
+  if (Hq % Hkv) return fail(OFFQ_ERR_INVALID, "Hq = %lld is not a multiple of Hkv = %lld",
+                            (long long)Hq, (long long)Hkv);
+  if (!(sm_scale > 0.0f) || sm_scale > 1e30f) return fail(OFFQ_ERR_INVALID, "sm_scale must be > 0");
+  if (ldq < Hq * head_dim || ldq % 8 || ldo < Hq * head_dim || ldo % 8)
+    return fail(OFFQ_ERR_INVALID, "need ldq, ldo >= Hq head_dim, multiples of 8");
+  if (!paged_attention_sizes(M, B, Hq, Hkv, head_dim, max_new) ||
+      max_pages > (int64_t(1) << 30) / page_size || num_pages > (int64_t(1) << 31) - 1 ||
+      ldq > (int64_t(1) << 40) || ldo > (int64_t(1) << 40))
+    return fail(OFFQ_ERR_UNSUPPORTED, "sizes too large");
+  if (M == 0 || B == 0 || max_new == 0) return ok();  // empty: pointers may be NULL
+  if (!q || !q_starts || !seq_lens || !page_table || !out)
+    return fail(OFFQ_ERR_INVALID, "null pointer argument");
+  if (offq_status_t st = check_paged_pointers(k_codes, v_codes, kv_params)) return st;
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(q_starts, 4) || !aligned(seq_lens, 4) ||
+      !aligned(page_table, 4) || !aligned(workspace, 16))
+    return fail(OFFQ_ERR_INVALID, "misaligned pointer (q, out, workspace: 16 B; lengths: 4 B)");
+  const int64_t need = offq_kv_attention_paged_workspace_bytes(M, B, Hq, Hkv, head_dim, max_new);
+  if (need > 0 && (!workspace || workspace_bytes < need))
+    return fail(OFFQ_ERR_INVALID, "workspace of %lld bytes, need %lld",
+                (long long)(workspace ? workspace_bytes : 0), (long long)need);
+  if (overlap(q, 2 * ((M - 1) * ldq + Hq * head_dim), out, 2 * ((M - 1) * ldo + Hq * head_dim)))
+    return fail(OFFQ_ERR_INVALID, "out overlaps q");
+  if (offq_status_t st = check_device()) return st;
+  const offq::PagedCache c = {const_cast<uint8_t*>(k_codes), const_cast<uint8_t*>(v_codes),
+                              const_cast<int16_t*>(kv_params), num_pages, ilog2_pow2(page_size),
+                              (int)Hkv};
+  const offq::PagedAttentionArgs a = {q,          ldq,
+                                      (int)M,     (int)Hq,
+                                      q_starts,   seq_lens,
+                                      (int)B,     (int)(max_new < M ? max_new : M),
+                                      page_table, (int)max_pages,
+                                      sm_scale,   k_hadamard,
+                                      v_hadamard, out,
+                                      ldo};
+  return launched(offq::launch_kv_attention_paged(a, c, head_dim, static_cast<float*>(workspace),
+                                                  (hipStream_t)stream),
+                  "kv_attention_paged");
 }
 
 int64_t offq_top1_workspace_bytes(int64_t n_seq, int64_t seq_len) {

@@ -1,0 +1,587 @@
+"""GPU parity: the paged 4-bit cache (offq_rope_kv_paged, offq_kv_dequantize_paged,
+offq_kv_attention_paged) against oracle/paged.py in fp64.
+
+Bars, with u = 2^-24 (fp32), 2^-11 (fp16), 2^-8 (bf16), half a step each:
+* query: the norm is a sum of D squares and three roundings a channel, the angle is exact to
+  2^-24 of a turn (sin, cos off by 2^-22), the rotation two products and a sum:
+  |q - q64| <= 2^-8 |q64| + (D / 2 + 16) 2^-24 |w| (|x_a| + |x_b|) rounded up to
+  2^-8 |q64| + D 2^-24 * max(row);
+* key or value before its codes: the same error and L = log2 D butterfly stages,
+  delta = (D + 16) 2^-24 sum_d |x_d| / sqrt(D) (no rotation: the row's largest in place of the
+  sum); without norm, rotation and Hadamard y is the input and the row is bit-exact.  The scale is
+  the fp16 rounding of a range off by at most 2 delta, the zero-point of a quotient off by
+  delta / s + 2^-20 |z|, a code of one off by as much again.
+* rows read back: s (c - z) is one product, the butterflies as above, one bf16 rounding.
+* attention: the rotated query enters in fp16 and so do scaled codes: a score is off by at most
+  2^-11 eta; weights and values have one fp16 rounding each and a value's zero-point term another:
+  |o - o64| <= 2^-8 (1 + 2^-5) |o64| + (2 eta + 4) 2^-11 (1 + 2^-4) E  per channel; times sqrt(D)
+  in the second term where the sum is rotated back (a row of H has D entries of 1 / sqrt(D)).
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2606_07116_amd as offq
+from oracle import paged as OP
+from oracle import quantizer as OQ
+from paper_2606_07116_amd import inputs
+from tests import parity as P
+
+pytestmark = pytest.mark.gpu
+
+DEV = P.DEV
+
+
+def _t(a, dtype=None):
+    t = torch.from_numpy(np.ascontiguousarray(a))
+    return (t if dtype is None else t.to(dtype)).to(DEV)
+
+
+def _bf16(rng, *shape, scale=1.0):
+    return inputs.round_to_bf16((scale * rng.standard_normal(shape)).astype(np.float32))
+
+
+def _host_cache(rng, pages, Hkv, P_, D, offsets=0):
+    """Codes over the whole grid, scales 0.05 .. 0.6, zero-points 3 .. 12, shifted by up to
+    `offsets` (rows around a large offset)."""
+    kc, vc = (rng.integers(0, 256, (pages, Hkv, P_, D // 2), dtype=np.uint8) for _ in range(2))
+    par = np.empty((pages, Hkv, P_, 4), np.int16)
+    par[..., ::2] = rng.uniform(0.05, 0.6, (pages, Hkv, P_, 2)).astype(np.float16).view(np.int16)
+    par[..., 1::2] = rng.integers(3, 13, (pages, Hkv, P_, 2))
+    if offsets:
+        par[..., 1::2] += rng.integers(-offsets, offsets + 1, (pages, Hkv, P_, 2), dtype=np.int16)
+    return kc, vc, par
+
+
+def _cache(kc, vc, par):
+    return dict(k_codes=_t(kc), v_codes=_t(vc), kv_params=_t(par))
+
+
+def _back(cache):
+    return P.host(cache["k_codes"]), P.host(cache["v_codes"]), P.host(cache["kv_params"])
+
+
+# ------------------------------------------------------------------ the write
+def _check_rows(codes, scale, zero, y, delta, exact):
+    """codes [.., D], scale, zero [..] of the rows y [.., D] known to within delta [..]."""
+    if exact:
+        q, s, z = OQ.quantize_groups(y.reshape(-1, y.shape[-1]).astype(np.float32), y.shape[-1])
+        assert np.array_equal(codes.reshape(q.shape), q)
+        assert np.array_equal(scale.reshape(-1), s.reshape(-1).astype(np.float64))
+        assert np.array_equal(zero.reshape(-1), z.reshape(-1).astype(np.float64))
+        return
+    mx, mn = y.max(-1), y.min(-1)
+    lo = (mx - mn - 2 * delta) / 15 * (1 - 2.0 ** -11 - 2.0 ** -22)
+    hi = (mx - mn + 2 * delta) / 15 * (1 + 2.0 ** -11 + 2.0 ** -22)
+    assert np.all((lo <= scale) & (scale <= hi))
+    off = delta / scale + 2.0 ** -20 * (np.abs(zero) + 16)
+    assert np.all(np.abs(zero + mn / scale) <= 0.5 + off)
+    want = y / scale[..., None] + zero[..., None]
+    inside = np.clip(want, 0, 15)
+    assert np.all(np.abs(codes - inside) <= 0.5 + 2 * off[..., None])
+
+
+def _write_case(M, Hq, Hkv, D, P_, rotary, pairs, norm, k_had, v_had, seed, ldq=0, ldo=0, far=0,
+                amplitude=1.0):
+    rng = np.random.default_rng(seed)
+    pages = M // P_ + 4
+    x = _bf16(rng, M, Hq + 2 * Hkv, D)
+    x[:, Hq:Hq + Hkv, D // 3] += inputs.round_to_bf16(np.float32(30.0))
+    x = inputs.round_to_bf16(x)
+    pos = (far + rng.integers(0, 5000, M)).astype(np.int32)
+    slots = rng.permutation(pages * P_)[:M].astype(np.int64)
+    slots[M // 2::7] = [-1, pages * P_, 1 << 40, -(1 << 40)][seed % 4]
+    freq = OP.inv_freq(rotary, 500000.0, 8.0, 1, 4, 8192).astype(np.float32) if rotary else None
+    qw, kw = (_bf16(rng, D) if norm else None for _ in range(2))
+    before = _host_cache(rng, pages, Hkv, P_, D)
+    cache = _cache(*before)
+    rows = P.to_dev_bf16(x.reshape(M, -1))
+    if ldq:
+        wide = torch.full((M, rows.shape[1] + ldq), 7.0, dtype=torch.bfloat16, device=DEV)
+        wide[:, :rows.shape[1]] = rows
+        rows = wide[:, :rows.shape[1]]
+    out = None
+    if ldo:
+        full = torch.full((M, Hq * D + ldo), 5.0, dtype=torch.bfloat16, device=DEV)
+        out = full[:, :Hq * D].unflatten(1, (Hq, D))
+    q = offq.offq_rope_kv_paged(rows, Hq, _t(pos), _t(slots), cache,
+                                None if freq is None else _t(freq), interleaved=pairs,
+                                amplitude=amplitude,
+                                q_weight=None if qw is None else P.to_dev_bf16(qw),
+                                k_weight=None if kw is None else P.to_dev_bf16(kw), eps=1e-6,
+                                k_hadamard=k_had, v_hadamard=v_had, out=out)
+    torch.cuda.synchronize()
+    if ldo:
+        assert bool((full[:, Hq * D:] == 5.0).all())
+
+    def turned(t, w):
+        t = OP.norm(t, w, 1e-6)
+        return OP.rotate(t, pos, freq, pairs, amplitude) if rotary else t
+
+    qr, kr = turned(x[:, :Hq], qw), turned(x[:, Hq:Hq + Hkv], kw)
+    vr = np.float64(x[:, Hq + Hkv:])
+    big = np.abs(qr).max(-1, keepdims=True) + np.abs(OP.norm(x[:, :Hq], qw, 1e-6)).max(-1, keepdims=True)
+    got = P.host(q.float()).astype(np.float64)
+    assert np.all(np.abs(got - qr) <= 2.0 ** -8 * np.abs(qr) + D * 2.0 ** -24 * big)
+    # the rows in their slots; everything else as it was
+    kc, vc, par = _back(cache)
+    ok = (slots >= 0) & (slots < pages * P_)
+    assert ok.any() or M == 1
+    for value, codes, had, y0 in ((False, kc, k_had, kr), (True, vc, v_had, vr)):
+        c, s, z = OP.rows(codes, par, slots[ok], value=value)
+        y = OP.hadamard_rows(y0[ok], had)
+        mag = np.abs(y0[ok])
+        delta = (D + 16) * 2.0 ** -24 * (mag.sum(-1) / math.sqrt(D) if had else 2 * mag.max(-1))
+        plain = not had and (value or (not norm and not rotary))
+        _check_rows(c, s, z, y, delta, plain)
+    touched = np.zeros(pages * P_, bool)
+    touched[slots[ok]] = True
+    keep = ~touched.reshape(pages, P_).transpose(0, 1)
+    for a, b in zip((kc, vc, par), before):
+        assert np.array_equal(a.transpose(0, 2, 1, 3)[keep], b.transpose(0, 2, 1, 3)[keep])
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("M,Hq,Hkv", [(1, 4, 1), (2, 32, 8), (37, 5, 1), (130, 6, 2), (300, 3, 3)])
+def test_write_shapes(M, Hq, Hkv, D):
+    _write_case(M, Hq, Hkv, D, 16, D, False, False, True, False, seed=M + D + Hq)
+
+
+@pytest.mark.parametrize("rotary", [0, 16, 48, 64, 96, 128])
+@pytest.mark.parametrize("pairs", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+def test_write_rotary(rotary, pairs, D):
+    if rotary > D:
+        pytest.skip("more rotated channels than the head has")
+    _write_case(29, 4, 2, D, 32, rotary, pairs, True, True, True, seed=rotary + D, amplitude=1.25)
+
+
+@pytest.mark.parametrize("norm,k_had,v_had", [(False, False, False), (True, False, True),
+                                              (True, True, False)])
+@pytest.mark.parametrize("rotary", [0, 128])
+def test_write_options(norm, k_had, v_had, rotary):
+    _write_case(41, 4, 2, 128, 64, rotary, False, norm, k_had, v_had, seed=rotary + 1)
+
+
+def test_write_far_positions_strides_many_tokens():
+    _write_case(1300, 8, 2, 128, 256, 128, False, True, True, False, seed=4, far=900000000, ldq=24,
+                ldo=8)
+    _write_case(700, 2, 1, 64, 4096, 32, True, False, True, True, seed=5, far=-1000, ldq=8, ldo=64)
+
+
+def test_write_degenerate_rows():
+    """Zero and constant rows, and a page size above the tokens."""
+    x = torch.zeros((3, 3 * 64), dtype=torch.bfloat16, device=DEV)
+    x[1] = 3.0
+    x[2, 64:128] = -2.0
+    cache = offq.paged_cache(2, 1, 128, 64, device=DEV)
+    slots = torch.tensor([7, 130, 255], device=DEV)
+    w = torch.ones(64, dtype=torch.bfloat16, device=DEV)
+    q = offq.offq_rope_kv_paged(x, 1, torch.zeros(3, dtype=torch.int32, device=DEV), slots, cache,
+                                q_weight=w, k_weight=w, eps=0.0 + 1e-6, k_hadamard=False)
+    k, v = offq.offq_kv_dequantize_paged(cache, slots, k_hadamard=False)
+    torch.cuda.synchronize()
+    assert not q[0].any() and not k[0].any() and not v[0].any() and not v[2].any()
+    assert bool((v[1] == 3.0).all()) and bool((k[2].float() + 1).abs().max() < 1e-2)
+    # eps = 0 on a zero row divides 0 by 0: the codes are unspecified, the others' are not
+    offq.offq_rope_kv_paged(x, 1, torch.zeros(3, dtype=torch.int32, device=DEV), slots, cache,
+                            q_weight=w, k_weight=w, eps=0.0, k_hadamard=False)
+    k, _ = offq.offq_kv_dequantize_paged(cache, slots, k_hadamard=False)
+    torch.cuda.synchronize()
+    assert bool((k[2].float() + 1).abs().max() < 1e-2)
+
+
+# ------------------------------------------------------------------ the read
+@pytest.mark.parametrize("M,Hkv,D,P_", [(1, 1, 64, 16), (3, 8, 128, 16), (77, 5, 64, 32),
+                                        (1000, 2, 128, 128), (5, 1, 128, 4096)])
+@pytest.mark.parametrize("k_had,v_had", [(True, False), (False, True)])
+def test_read(M, Hkv, D, P_, k_had, v_had):
+    rng = np.random.default_rng(M + Hkv)
+    pages = 5
+    host = _host_cache(rng, pages, Hkv, P_, D, offsets=3000)
+    slots = rng.integers(0, pages * P_, M).astype(np.int64)  # repeats among them
+    slots[2::5] = [-1, pages * P_, 1 << 45][M % 3]
+    out = [torch.full((M, Hkv * D + 8), 9.0, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    k, v = offq.offq_kv_dequantize_paged(_cache(*host), _t(slots), k_had, v_had,
+                                         *(o[:, :Hkv * D].unflatten(1, (Hkv, D)) for o in out))
+    torch.cuda.synchronize()
+    ok = (slots >= 0) & (slots < pages * P_)
+    for got, codes, value, had in ((k, host[0], False, k_had), (v, host[1], True, v_had)):
+        ref = OP.dequantize(codes, host[2], slots[ok], value, had)
+        raw = np.abs(OP.dequantize(codes, host[2], slots[ok], value))
+        lim = 2.0 ** -8 * np.abs(ref) * (1 + 2.0 ** -7) + 2.0 ** -24 * (
+            10 * raw.sum(-1, keepdims=True) / math.sqrt(D) if had else 2 * raw.max(-1, keepdims=True))
+        g = P.host(got.float()).astype(np.float64)
+        assert np.all(np.abs(g[ok] - ref) <= lim)
+        assert np.all(g[~ok] == 9.0)
+    assert bool((out[0][:, -8:] == 9.0).all()) and bool((out[1][:, -8:] == 9.0).all())
+
+
+def test_read_one_side_and_rows_side_by_side():
+    rng = np.random.default_rng(8)
+    host = _host_cache(rng, 3, 2, 16, 64)
+    cache, slots = _cache(*host), _t(np.arange(48))
+    k, v = offq.offq_kv_dequantize_paged(cache, slots)
+    both = torch.zeros((48, 2, 2, 64), dtype=torch.bfloat16, device=DEV)
+    offq.offq_kv_dequantize_paged(cache, slots, k_out=both[:, 0], v_out=both[:, 1])
+    from paper_2606_07116_amd import _lib
+    one = torch.zeros_like(k)
+    ptrs = [cache[n].data_ptr() for n in ("k_codes", "v_codes", "kv_params")]
+    assert _lib.offq_kv_dequantize_paged_raw(*ptrs, 3, 16, 2, 64, slots.data_ptr(), 48, 1, 0, None, 0,
+                                             one.data_ptr(), 128, None) == _lib.OFFQ_OK
+    torch.cuda.synchronize()
+    assert torch.equal(both[:, 0], k) and torch.equal(both[:, 1], v) and torch.equal(one, v)
+
+
+# ------------------------------------------------------------------ attention
+def _tables(rng, lens, P_, width=None, spare=2):
+    need = [-(-max(n, 0) // P_) for n in lens]
+    pages = sum(need) + spare
+    perm = rng.permutation(pages)
+    table = np.full((len(lens), width or max(need + [1]) + 1), -1, np.int32)
+    at = 0
+    for b, n in enumerate(need):
+        table[b, :n] = perm[at:at + n]
+        at += n
+    return table, pages
+
+
+def _attend(new, past, Hq, Hkv, D, P_, seed, k_had=True, v_had=False, sm=None, offsets=0, edit=None,
+            max_new=None, lead=0, tail=0, ld=0, sample=None, qscale=1.0):
+    """Sequences of new[b] rows after past[b] positions against the oracle; the pages hold
+    poisoned rows wherever no position is; `edit` changes (table, host cache, lens)."""
+    rng = np.random.default_rng(seed)
+    lens = [n + p for n, p in zip(new, past)]
+    table, pages = _tables(rng, lens, P_)
+    host = _host_cache(rng, pages, Hkv, P_, D, offsets)
+    used = np.zeros((pages, P_), bool)
+    for b, n in enumerate(lens):
+        for j in range(n):
+            used[table[b, j // P_], j % P_] = True
+    bad = ~used
+    host[2].transpose(0, 2, 1, 3)[bad] = np.array([np.float16(np.nan).view(np.int16), -30000,
+                                                   np.float16(np.inf).view(np.int16), 30000])
+    lens = np.array(lens, np.int32)
+    if edit:
+        edit(table, host, lens)
+    M = sum(new) + lead + tail
+    starts = (lead + np.concatenate([[0], np.cumsum(new)])).astype(np.int32)
+    q = _bf16(rng, M, Hq, D, scale=qscale)
+    sm = 1 / math.sqrt(D) if sm is None else sm
+    qd = torch.full((M, Hq * D + ld), float("nan"), dtype=torch.bfloat16, device=DEV)
+    qd[:, :Hq * D] = P.to_dev_bf16(q.reshape(M, -1))
+    out = torch.full((M, Hq * D + ld), 77.0, dtype=torch.bfloat16, device=DEV)
+    head = lambda t: t[:, :Hq * D].unflatten(1, (Hq, D))  # noqa: E731
+    args = (head(qd), _t(starts), _t(lens), _t(table), _cache(*host),
+            max(new + [0]) if max_new is None else max_new)
+    offq.offq_kv_attention_paged(*args, sm_scale=sm, k_hadamard=k_had, v_hadamard=v_had,
+                                 out=head(out))
+    torch.cuda.synchronize()
+    got = P.host(head(out).float()).astype(np.float64)
+    assert bool((out[:, Hq * D:] == 77.0).all())
+    ref, E, eta, written = OP.attention(q, starts, lens, table, *host, sm, k_had, v_had,
+                                        max_new=max_new)
+    assert np.all(got[~written] == 77.0)
+    lim = 2.0 ** -8 * (1 + 2.0 ** -5) * np.abs(ref) + \
+        (2 * eta + 4) * 2.0 ** -11 * (1 + 2.0 ** -4) * E * (math.sqrt(D) if v_had else 1)
+    bad = np.abs(got - ref) > lim
+    bad[~written] = False
+    assert not bad.any(), (f"{bad.sum()} of {bad.size} at {np.argwhere(bad)[:4].tolist()}: "
+                           f"gpu {got[bad][:4]} ref {ref[bad][:4]} lim {lim[bad][:4]}")
+    assert not got[written & ~E.any((1, 2))].any()  # rows that see nothing
+    return args, out, got
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("G", [1, 2, 3, 4, 5, 7, 8, 16, 20])
+def test_decode_groups(G, D):
+    _attend([1, 1, 1], [0, 37, 250], 2 * G, 2, D, 16, seed=G + D)
+
+
+@pytest.mark.parametrize("past", [0, 1, 14, 15, 16, 31, 32, 63, 64, 127, 128, 255, 511, 1023, 1500])
+def test_decode_lengths(past):
+    _attend([1], [past], 4, 1, 128, 16, seed=past, v_had=past % 2 == 1)
+
+
+@pytest.mark.parametrize("P_", [16, 32, 64, 256, 4096])
+def test_page_sizes(P_):
+    _attend([1, 3, 70], [P_ - 1, 2 * P_ % 700, 17], 4, 2, 128, P_, seed=P_)
+
+
+def test_decode_ragged_batch():
+    rng = np.random.default_rng(3)
+    past = rng.integers(0, 900, 40).tolist()
+    past[3] = 4000
+    _attend([1] * 40, past, 8, 2, 128, 32, seed=3)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("new,past", [
+    ([2, 5, 1], [100, 3, 0]), ([8] * 3, [511, 0, 64]), ([17], [40]), ([33, 1], [0, 200]),
+    ([64], [64]), ([65, 129], [0, 31]), ([200, 1, 0, 3], [300, 0, 9, 77]), ([1, 300], [900, 0]),
+])
+def test_chunks(new, past, D):
+    _attend(new, past, 8, 2, D, 16, seed=sum(new) + D)
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (6, 2), (5, 1), (16, 1), (7, 7)])
+def test_prompt_heads(Hq, Hkv):
+    _attend([90, 41], [0, 0], Hq, Hkv, 128, 32, seed=Hq, v_had=Hq % 2 == 0)
+
+
+@pytest.mark.parametrize("k_had,v_had", [(False, False), (False, True), (True, True)])
+@pytest.mark.parametrize("new,past", [([1, 4], [300, 7]), ([70], [20])])
+def test_rotations(k_had, v_had, new, past):
+    _attend(new, past, 4, 2, 64, 16, seed=1, k_had=k_had, v_had=v_had)
+
+
+@pytest.mark.parametrize("sm", [1e-4, 0.02, 0.6, 4.0])
+@pytest.mark.parametrize("new,past", [([1, 2], [700, 40]), ([80], [100])])
+def test_score_scales(sm, new, past):
+    _attend(new, past, 4, 1, 128, 16, seed=2, sm=sm)
+
+
+@pytest.mark.parametrize("offsets", [40, 3000, 30000])
+@pytest.mark.parametrize("new,past", [([1, 3], [300, 90]), ([75], [60])])
+def test_large_zero_points(offsets, new, past):
+    """Rows around an offset far from zero (what the rotation's first channel leaves)."""
+    def small(table, host, lens):  # keeps the scores of offset rows apart by a few units only
+        used = host[2][..., 1] != -30000
+        host[2][..., 0][used] = np.float16(0.3 * 12 / offsets).view(np.int16)
+
+    _attend(new, past, 4, 2, 128, 16, seed=offsets, offsets=offsets, edit=small)
+
+
+@pytest.mark.parametrize("new,past", [([1, 4], [500, 33]), ([66], [200])])
+def test_scales_far_apart(new, past):
+    """Value scales from 2^-24 to 60000 along the sequence, key scales over four decades."""
+    def spread(table, host, lens):
+        rng = np.random.default_rng(1)
+        used = host[2][..., 1] != -30000
+        n = int(used.sum())
+        host[2][..., 2][used] = np.exp(rng.uniform(np.log(2.0 ** -24), np.log(60000), n)).astype(
+            np.float16).view(np.int16)
+        host[2][..., 0][used] = np.exp(rng.uniform(np.log(1e-4), np.log(0.5), n)).astype(
+            np.float16).view(np.int16)
+
+    _attend(new, past, 4, 2, 128, 16, seed=6, edit=spread)
+
+
+@pytest.mark.parametrize("new,past", [([1, 4], [500, 33]), ([66], [200])])
+def test_zero_scales(new, past):
+    """Rows that were never written (all zero) inside a sequence: values 0, scores 0."""
+    def blank(table, host, lens):
+        host[2][table[0, 0]] = 0
+
+    _attend(new, past, 4, 2, 128, 16, seed=7, edit=blank)
+
+
+@pytest.mark.parametrize("new,past", [([1, 4, 2], [500, 33, 64]), ([66, 1], [200, 90])])
+def test_absent_pages(new, past):
+    """Pages missing at the front, in the middle, and for a whole sequence."""
+    def drop(table, host, lens):
+        table[0, [0, 2, 3]] = [-1, 1 << 30, -(1 << 31)]
+        table[1] = -5
+
+    args, _, got = _attend(new, past, 4, 2, 128, 16, seed=8, edit=drop)
+    assert not got[new[0]:new[0] + new[1]].any()
+
+
+@pytest.mark.parametrize("new,past", [([1, 5, 1], [300, 33, 12]), ([90, 20], [200, 0])])
+def test_lengths_that_leave_rows_empty(new, past):
+    """A sequence shorter than its rows, an empty one, a length past the table, a negative one."""
+    def cut(table, host, lens):
+        lens[1] = new[1] - 3
+        if len(lens) > 2:
+            lens[0], lens[2] = -4, 1 << 30
+            used = host[2][table[2][table[2] >= 0]]
+            used[..., 0] = used[..., 2] = np.float16(0.25).view(np.int16)
+            used[..., 1::2] = 7
+            host[2][table[2][table[2] >= 0]] = used
+
+    _attend(new, past, 4, 2, 128, 16, seed=9, edit=cut)
+
+
+def test_padded_rows_and_max_new():
+    _attend([1, 2, 3], [40, 0, 9], 4, 2, 64, 16, seed=10, lead=3, tail=5, ld=16)
+    _attend([70, 2], [40, 600], 4, 2, 128, 16, seed=11, lead=1, tail=70, ld=8)
+    _attend([5, 2, 9], [40, 0, 9], 4, 2, 128, 16, seed=12, max_new=3)
+    _attend([90, 2], [40, 0], 4, 2, 128, 16, seed=13, max_new=40)
+    _attend([1, 1], [40, 0], 4, 2, 128, 16, seed=14, max_new=1000)
+
+
+def test_long_context_few_rows():
+    """The keys split over many workgroups and joined again."""
+    _attend([1, 2], [20000, 3], 4, 1, 128, 64, seed=15)
+    _attend([40], [9000], 4, 1, 128, 16, seed=16)
+
+
+def test_repeatable_and_on_another_stream():
+    for new, past in (([1] * 5, [700] * 5), ([60, 3], [300, 2000])):
+        args, out, got = _attend(new, past, 8, 2, 128, 16, seed=17)
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            a = offq.offq_kv_attention_paged(*args)
+            b = offq.offq_kv_attention_paged(*args)
+        s.synchronize()
+        assert torch.equal(a, b)
+        assert np.array_equal(P.host(a.float()), got.astype(np.float32))
+
+
+def test_offsets_past_32_bits():
+    """Pages beyond 4 GiB of codes: written, read back, attended to."""
+    Hkv, D, P_ = 8, 128, 256
+    pages = (5 << 30) // (Hkv * P_ * D // 2)
+    cache = {"k_codes": torch.empty((pages, Hkv, P_, D // 2), dtype=torch.uint8, device=DEV),
+             "v_codes": torch.empty((pages, Hkv, P_, D // 2), dtype=torch.uint8, device=DEV),
+             "kv_params": torch.empty((pages, Hkv, P_, 4), dtype=torch.int16, device=DEV)}
+    small = offq.paged_cache(3, Hkv, P_, D, device=DEV)
+    rng = np.random.default_rng(18)
+    M = 300
+    x = P.to_dev_bf16(_bf16(rng, M, (8 + 2 * Hkv) * D))
+    pos = _t(np.arange(M, dtype=np.int32))
+    far, near = np.array([pages - 1, pages - 7]), np.array([2, 0])
+    f = offq.offq_rope_inv_freq(D, device=DEV)
+    got = []
+    for c, t in ((cache, far), (small, near)):
+        slots = _t(t[np.arange(M) // P_] * P_ + np.arange(M) % P_)
+        q = offq.offq_rope_kv_paged(x, 8, pos, slots, c, f)
+        o = offq.offq_kv_attention_paged(
+            q, _t(np.array([0, M], np.int32)), _t(np.array([M], np.int32)),
+            _t(t[None].astype(np.int32)), c, M)
+        d = offq.offq_kv_attention_paged(
+            q[-1:], _t(np.array([0, 1], np.int32)), _t(np.array([M], np.int32)),
+            _t(t[None].astype(np.int32)), c, 1)
+        got.append((q, o, d, *offq.offq_kv_dequantize_paged(c, slots)))
+    torch.cuda.synchronize()
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+
+
+# ------------------------------------------------------------------ together
+def _serve(steps, graph):
+    """Two sequences through the cache: a prompt each, then single tokens; the queries' outputs
+    of every step and the cache's values at the end."""
+    Hq, Hkv, D, P_, width = 8, 2, 128, 16, 12
+    torch.manual_seed(0)
+    cache = offq.paged_cache(2 * width, Hkv, P_, D, device=DEV)
+    table = torch.randperm(2 * width, device=DEV).view(2, width).int()
+    f = offq.offq_rope_inv_freq(D, factor=4.0, original_len=8192, device=DEV)
+    w = [torch.rand(D, device=DEV).bfloat16() + 0.5 for _ in range(2)]
+
+    def slots(b, p):
+        return table[b, p // P_].long() * P_ + p % P_
+
+    def step(x, b, p, starts, lens, max_new):
+        q = offq.offq_rope_kv_paged(x, Hq, p.int(), slots(b, p), cache, f, q_weight=w[0],
+                                    k_weight=w[1])
+        return offq.offq_kv_attention_paged(q, starts, lens, table, cache, max_new)
+
+    new = (37, 70)
+    b = torch.repeat_interleave(torch.arange(2, device=DEV), torch.tensor(new, device=DEV))
+    p = torch.cat([torch.arange(n, device=DEV) for n in new])
+    xs = [torch.randn((n, (Hq + 2 * Hkv) * D), device=DEV).bfloat16() for n in (107,) + (2,) * steps]
+    outs = [step(xs[0], b, p, torch.tensor([0, 37, 107], dtype=torch.int32, device=DEV),
+                 torch.tensor(new, dtype=torch.int32, device=DEV), 70)]
+    b, starts = torch.arange(2, device=DEV), torch.arange(3, dtype=torch.int32, device=DEV)
+    pos = torch.tensor(new, device=DEV)
+    if not graph:
+        for i in range(steps):
+            outs.append(step(xs[1 + i], b, pos + i, starts, (pos + i + 1).int(), 1))
+    else:
+        x, at = xs[1].clone(), pos.clone()
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            keep = {n: t.clone() for n, t in cache.items()}
+            step(x, b, at, starts, (at + 1).int(), 1)
+            for n, t in cache.items():
+                t.copy_(keep[n])
+        torch.cuda.current_stream().wait_stream(side)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            o = step(x, b, at, starts, (at + 1).int(), 1)
+        for i in range(steps):
+            x.copy_(xs[1 + i])
+            at.copy_(pos + i)
+            g.replay()
+            outs.append(o.clone())
+            torch.cuda.synchronize()
+    lens = [n + steps for n in new]
+    at = [torch.arange(n, device=DEV) for n in lens]
+    values = [offq.offq_kv_dequantize_paged(cache, slots(i, a)) for i, a in enumerate(at)]
+    torch.cuda.synchronize()
+    return outs, values, xs
+
+
+def test_prompt_then_single_tokens_as_one_prompt():
+    """Tokens one at a time leave what the whole prompt leaves: the same cache bit for bit, and
+    outputs that agree to the two calls' roundings."""
+    outs, values, xs = _serve(9, graph=False)
+    Hq, Hkv, D, P_ = 8, 2, 128, 16
+    torch.manual_seed(0)
+    cache = offq.paged_cache(24, Hkv, P_, D, device=DEV)
+    table = torch.randperm(24, device=DEV).view(2, 12).int()
+    f = offq.offq_rope_inv_freq(D, factor=4.0, original_len=8192, device=DEV)
+    w = [torch.rand(D, device=DEV).bfloat16() + 0.5 for _ in range(2)]
+    steps = torch.stack(xs[1:])
+    x = torch.cat([xs[0][:37], steps[:, 0], xs[0][37:], steps[:, 1]])
+    b = torch.repeat_interleave(torch.arange(2, device=DEV), torch.tensor([46, 79], device=DEV))
+    p = torch.cat([torch.arange(46, device=DEV), torch.arange(79, device=DEV)])
+    s = table[b, p // P_].long() * P_ + p % P_
+    q = offq.offq_rope_kv_paged(x, Hq, p.int(), s, cache, f, q_weight=w[0], k_weight=w[1])
+    o = offq.offq_kv_attention_paged(q, torch.tensor([0, 46, 125], dtype=torch.int32, device=DEV),
+                                     torch.tensor([46, 79], dtype=torch.int32, device=DEV), table,
+                                     cache, 79)
+    for i, sl in enumerate((s[:46], s[46:])):
+        for a, c in zip(offq.offq_kv_dequantize_paged(cache, sl), values[i]):
+            assert torch.equal(a, c)
+    single = torch.stack(outs[1:]).float()  # [steps, 2, Hq, D]
+    whole = torch.stack([o[37:46], o[116:125]], 1).float()
+    torch.cuda.synchronize()
+    # values are below 8 in size: two bf16 roundings and the fp16 ones of both calls
+    assert float((single - whole).abs().max()) <= 2 * 8 * (2.0 ** -8 + 8 * 2.0 ** -11)
+    assert float(whole.abs().max()) > 0.1
+
+
+def test_captured_step_replays_with_new_lengths():
+    a, va, _ = _serve(6, graph=False)
+    b, vb, _ = _serve(6, graph=True)
+    for x, y in zip(a, b):
+        assert torch.equal(x, y)
+    for x, y in zip(va, vb):
+        assert torch.equal(x[0], y[0]) and torch.equal(x[1], y[1])
+
+
+def test_wrapper_refusals():
+    cache = offq.paged_cache(4, 2, 16, 64, device=DEV)
+    q = torch.zeros((3, 4, 64), dtype=torch.bfloat16, device=DEV)
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device=DEV)  # noqa: E731
+    table = torch.zeros((1, 2), dtype=torch.int32, device=DEV)
+    good = (q, i32(0, 3), i32(3), table, cache, 3)
+    offq.offq_kv_attention_paged(*good)
+    for at, wrong, err in ((0, q.float(), TypeError), (0, q[:, :3], ValueError),
+                           (1, i32(0, 1, 3), ValueError), (2, i32(3).long(), TypeError),
+                           (3, table.cpu(), ValueError), (3, table.repeat(2, 1), ValueError)):
+        with pytest.raises((err, offq.OffqError)):
+            offq.offq_kv_attention_paged(*good[:at], wrong, *good[at + 1:])
+    need = offq.offq_kv_attention_paged_workspace_bytes(3, 1, 4, 2, 64, 3)
+    if need:
+        with pytest.raises(offq.OffqError):
+            offq.offq_kv_attention_paged(*good, workspace=torch.empty(
+                need - 4, dtype=torch.uint8, device=DEV))
+    with pytest.raises(offq.OffqError):
+        offq.offq_kv_attention_paged(*good, out=q)
+    with pytest.raises(ValueError):
+        offq.offq_kv_attention_paged(*good[:4], {**cache, "kv_params": cache["kv_params"][:3]}, 3)
+    x = torch.zeros((3, 8 * 64), dtype=torch.bfloat16, device=DEV)
+    slots = torch.zeros(3, dtype=torch.int64, device=DEV)
+    for bad in ((x[:, :-8], 4, i32(0, 1, 2), slots), (x, 4, i32(0, 1), slots),
+                (x, 4, i32(0, 1, 2), slots.int())):
+        with pytest.raises((ValueError, TypeError)):
+            offq.offq_rope_kv_paged(*bad, cache)
+    with pytest.raises(TypeError):
+        offq.offq_kv_dequantize_paged(cache, slots.int())
