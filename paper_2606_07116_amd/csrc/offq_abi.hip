@@ -577,7 +577,7 @@ bool paged_attention_sizes(int64_t M, int64_t B, int64_t Hq, int64_t Hkv, int32_
                            int64_t max_new) {
   return M >= 0 && B >= 0 && max_new >= 0 && Hq > 0 && Hkv > 0 && Hq % Hkv == 0 &&
          (head_dim == 64 || head_dim == 128) && M <= (1 << 24) && B <= (1 << 20) &&
-         Hq <= (1 << 12) && M * Hq <= (int64_t(1) << 31) && B * Hkv <= (1 << 22);
+         Hq <= (1 << 12) && M * Hq <= (int64_t(1) << 30) && B * Hkv <= (1 << 22);
 }
 }  // namespace
 

@@ -591,163 +591,619 @@ __global__ __launch_bounds__(256) void kv_attention_paged_join_kernel(
   store_row<D>(a, j.q0 + row / G, hk * G + row % G, o, l, lane);
 }
 
-// One wave per (query row, head): 64 positions at a time, a lane first holding one position's
-// score, then D / 64 channels of the output.
+// ---------------------------------------------------------------------------
+// Many rows: tiles of 256 query rows (new tokens x heads of a group) of a sequence and
+// key/value head, eight waves of 32 rows, over blocks of 64 positions.  With many queries per
+// key the products bound it, so both run as 32x32x16 fp16 matrix products and everything that
+// can leave the score loop does:
+// * a block's codes become fp16 values once per workgroup, on their way to LDS: keys A c with
+//   A = sk 2^-E (a power of two per block), values A (c - z) with A = sv 2^-F (F follows the
+//   largest sv (16 + |z|) met), one rounding each (2^-11; a value's zero-point term another).  Per
+//   weight there is no scale, no zero-point and no slope left to apply;
+// * the keys' zero-point term -z_j sum q, which can be far larger than the score, is a k-step of
+//   its own: A z_j and sum q as three fp16 pieces each, their six leading products;
+// * S^T = K Q^T: a lane holds 16 positions of one query row per tile of 32, so maximum and sum
+//   stay in the lane, and the tile is in the operand layout of O^T = V^T P^T; V^T lies in LDS with
+//   the positions in the order of the accumulator and the channels as (nibble, code word), so
+//   that a lane ends with eight consecutive channels of each of its words;
+// * weights are 2^(s - m), m lagging so that they stay within [2^-24, 2^15] around 2^7; their sum
+//   is taken of the rounded ones.
+// Longest tiles start first.  Where the tiles do not fill the CUs, the keys of a tile are split
+// over workgroups and the rows joined by a second kernel.
+constexpr int ROWS = 256;      // query rows of a tile
+constexpr int KB = 64;         // positions of a block
+constexpr int VROW = 2 * KB + 16;
+constexpr float TOP = 15.0f;   // a weight 2^x may rise to x = 15 before its row's reference moves,
+constexpr float MID = 7.0f;    // to put the largest at x = 7
+
+typedef float f16_t __attribute__((ext_vector_type(16)));
+
 template <int D>
-__global__ __launch_bounds__(64) void kv_attention_paged_kernel(PagedAttentionArgs a, PagedCache c,
-                                                               int few_rows) {
-  constexpr int E = D / 64;
-  __shared__ float s_q[D];
-  __shared__ float s_p[64];
-  __shared__ int64_t s_row[64];
-  const int lane = (int)__builtin_amdgcn_workitem_id_x();
-  const int m = (int)__builtin_amdgcn_workgroup_id_x(), hq = (int)__builtin_amdgcn_workgroup_id_y();
-  // the sequence of row m: the last b with q_starts[b] <= m
-  int b = 0;
-  for (int hi = a.B; hi - b > 1;) {
-    const int mid = (b + hi) / 2;
-    if (a.q_starts[mid] <= m) b = mid;
-    else hi = mid;
+struct alignas(16) Stage {
+  uint8_t k[KB * (2 * D + 16)];  // per position: A c, 8 fp16 per code word, in operand order
+  uint8_t v[D * VROW];           // per channel (nibble * D / 8 + word): A (c - z) of the 64 positions
+  uint4 z[KB];                   // per position: the pieces of A z
+  int E, F;
+  uint32_t valid[2];             // bit j: position j is seen (by rows past it)
+};
+
+__device__ __forceinline__ uint32_t pk_f16(float a, float b) {
+  const h2_t h = {(_Float16)a, (_Float16)b};
+  return __builtin_bit_cast(uint32_t, h);
+}
+__device__ __forceinline__ uint32_t pk_mul(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2_t, a) * __builtin_bit_cast(h2_t, b));
+}
+__device__ __forceinline__ uint32_t pk_fma(uint32_t a, uint32_t b, uint32_t c) {
+  return __builtin_bit_cast(uint32_t,
+                            __builtin_elementwise_fma(__builtin_bit_cast(h2_t, a), __builtin_bit_cast(h2_t, b),
+                                                      __builtin_bit_cast(h2_t, c)));
+}
+
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {
+  return __builtin_bit_cast(
+      float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+// the wave's largest value (of values >= 0), the same in every lane
+__device__ __forceinline__ float wave_top(float v) {
+  v = fmaxf(v, dpp<0x128>(v));  // rotations within rows of 16 lanes
+  v = fmaxf(v, dpp<0x124>(v));
+  v = fmaxf(v, dpp<0x122>(v));
+  v = fmaxf(v, dpp<0x121>(v));
+  const int i = __builtin_bit_cast(int, v);
+  const int a = max(__builtin_amdgcn_readlane(i, 0), __builtin_amdgcn_readlane(i, 16));
+  const int b = max(__builtin_amdgcn_readlane(i, 32), __builtin_amdgcn_readlane(i, 48));
+  return __builtin_bit_cast(float, max(a, b));
+}
+
+// x = h1 + h2 + h3 + O(2^-33 x): fp16 pieces
+struct Pieces {
+  float h1, h2, h3;
+};
+__device__ __forceinline__ Pieces pieces(float x) {
+  Pieces p;
+  p.h1 = (float)(_Float16)x;
+  p.h2 = (float)(_Float16)(x - p.h1);
+  p.h3 = (float)(_Float16)(x - p.h1 - p.h2);
+  return p;
+}
+
+struct Tile {
+  int b, i;  // sequence and tile within it
+  int index, count;
+  bool found;
+  Seq s;
+};
+// Tile number `t` of all sequences' tiles, counted from the last: the longest of a sequence first.
+__device__ __forceinline__ Tile find_tile(const PagedAttentionArgs& a, int log2p, int G, int few_rows,
+                                          int t) {
+  const int lane = (int)__builtin_amdgcn_workitem_id_x() & 63;
+  Seq s{};
+  auto load = [&](int b) {
+    s = Seq{};
+    if (b < a.B) s = sequence(a, log2p, G, b);
+    return s.rows > few_rows ? (s.rows + ROWS - 1) / ROWS : 0;
+  };
+  int count = 0, mine = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 64) count += mine = load(b0 + lane);
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) count += __shfl_xor(count, o);
+  Tile r{};
+  r.count = count;
+  if (t >= count) return r;
+  r.index = count - 1 - t;
+  int base = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    if (a.B > 64) mine = load(b0 + lane);
+    int incl = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int p = __shfl_up(incl, o);
+      if (lane >= o) incl += p;
+    }
+    const int first = base + incl - mine;
+    const uint64_t hit = __builtin_amdgcn_ballot_w64(r.index >= first && r.index < first + mine);
+    if (hit) {
+      const int o = __builtin_ctzll(hit);
+      r.found = true;
+      r.b = b0 + o;
+      r.i = r.index - __builtin_amdgcn_readlane(first, o);
+      r.s.q0 = __builtin_amdgcn_readlane(s.q0, o);
+      r.s.rows = __builtin_amdgcn_readlane(s.rows, o);
+      r.s.keys = __builtin_amdgcn_readlane(s.keys, o);
+      r.s.pos0 = __builtin_amdgcn_readlane(s.pos0, o);
+      return r;
+    }
+    base += __builtin_amdgcn_readlane(incl, 63);
   }
-  const int q0 = a.q_starts[b], n = a.q_starts[b + 1] - q0;
-  const int i = m - q0;
-  if (i < 0 || i >= n || i >= a.max_new) return;  // in no sequence
-  const int len = a.seq_lens[b];
-  const int G = a.Hq / c.Hkv, hk = hq / G;
-  if (min(n, a.max_new) * G <= few_rows) return;
-  const int64_t seen = min((int64_t)len - n + i + 1, (int64_t)a.max_pages << c.log2p);
-  const uint16_t* q = a.q + (int64_t)m * a.ldq + (int64_t)hq * D;
-  for (int e = 0; e < E; ++e) s_q[e * 64 + lane] = bf16_lo(q[e * 64 + lane]);
+  return r;
+}
+
+// The rows of a tile that the second kernel joins.
+struct alignas(16) TileJoint {
+  int q0, row0, rows, nsplit;
+};
+
+template <int D>
+__global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
+    PagedAttentionArgs a, PagedCache c, int few_rows, int splits, TileJoint* __restrict__ joints,
+    float* __restrict__ rec) {
+  constexpr int KROW = 2 * D + 16;
+  constexpr int NS = D / 16;   // k-steps of the score product
+  constexpr int ND = D / 32;   // tiles of output channels
+  constexpr int NV = D / 8;    // code words of a row
+  __shared__ Stage<D> st[2];
+  const int tid = (int)__builtin_amdgcn_workitem_id_x();
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int ql = lane & 31, h = lane >> 5;
+  const int G = a.Hq / c.Hkv;
+  const int id = (int)__builtin_amdgcn_workgroup_id_x();
+  const int split = id % splits, hk = id / splits % c.Hkv, t = id / splits / c.Hkv;
+  const Tile w = find_tile(a, c.log2p, G, few_rows, t);
+  if (!w.found) {
+    if (joints && !split && !hk && !tid) joints[t] = TileJoint{0, 0, 0, 0};
+    return;
+  }
+  const int row0 = w.i * ROWS;
+  const int last = min(w.s.rows, row0 + ROWS) - 1;  // the tile's last row
+  // the positions that its rows see, and this split's blocks of them
+  const int keys = (int)min((int64_t)max(w.s.pos0 + last / G + 1, 0), (int64_t)w.s.keys);
+  const int nblk = (keys + KB - 1) / KB;
+  const int ns = max(1, min(splits, nblk / 4));
+  if (joints && !split && !hk && !tid) joints[w.index] = TileJoint{w.s.q0, row0, last + 1 - row0, ns};
+  if (split >= ns) return;
+  const int kb0 = (int)((int64_t)nblk * split / ns), kb1 = (int)((int64_t)nblk * (split + 1) / ns);
+
+  // ---- this wave's rows
+  const int wrow = row0 + 32 * wave;
+  const bool live = wrow <= last;
+  const int row = min(wrow + ql, last);
+  const int tok = row / G, hq = hk * G + row - tok * G;
+  const int pos = w.s.pos0 + tok;
+  const int pmin = w.s.pos0 + wrow / G, pmax = w.s.pos0 + min(wrow + 31, last) / G;
+
+  // ---- staging: waves 0..3 16 positions of keys each, waves 4..7 of values
+  const int32_t* table = a.page_table + (int64_t)w.b * a.max_pages;
+  const int grp = wave & 3;
+  const bool vwave = wave >= 4;
+  int id0 = kb0 * KB, ids = -1;  // lane i: the page of the 16 positions from id0 + 16 i on
+  auto load_ids = [&]() {
+    const int key = id0 + 16 * lane;
+    ids = key < keys ? table[key >> c.log2p] : -1;
+  };
+  uint32_t code[4];
+  uint2 par;
+  bool ok;
+  int Fmax = -200;
+  auto load = [&](int kb) {
+    const int k0 = kb * KB;
+    if (k0 - id0 >= 1024) {
+      id0 = k0;
+      load_ids();
+    }
+    const int gi = (k0 - id0) >> 4, off = k0 & ((1 << c.log2p) - 1);
+    const int mask = (1 << c.log2p) - 1;
+    // this wave's group of codes
+    int pg = __builtin_amdgcn_readlane(ids, gi + grp);
+    if (pg < 0 || pg >= c.pages) pg = 0;
+    const int64_t r = c.row(pg, hk, (off + 16 * grp) & mask);
+    if (!vwave) {
+      const uint8_t* p = c.kc + r * (D / 2) + (uint32_t)((lane >> 2) * (D / 2) + (lane & 3) * (D / 8));
+      if constexpr (D == 128) {
+        const uint4 x = *reinterpret_cast<const uint4*>(p);
+        code[0] = x.x;
+        code[1] = x.y;
+        code[2] = x.z;
+        code[3] = x.w;
+      } else {
+        const uint2 x = *reinterpret_cast<const uint2*>(p);
+        code[0] = x.x;
+        code[1] = x.y;
+      }
+    } else {
+      const uint8_t* p = c.vc + r * (D / 2) +
+                         (uint32_t)(4 * (lane / NV % 4) * (D / 2) + 4 * (lane % NV));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) code[i] = *reinterpret_cast<const uint32_t*>(p + i * (D / 2));
+    }
+    // the parameters of position `lane` of the block
+    const int pl = __shfl(ids, gi + (lane >> 4));
+    ok = pl >= 0 && pl < c.pages && k0 + lane < keys;
+    par = *reinterpret_cast<const uint2*>(
+        c.par + 4 * c.row(ok ? pl : 0, hk, (off + (lane & 48)) & mask) + 4 * (lane & 15));
+  };
+  auto store = [&](Stage<D>& S) {
+    if (!vwave) {
+      const float sk = ok ? fp16_bits_to_f32((uint16_t)par.x) : 0.0f;
+      const int E = __builtin_amdgcn_frexp_expf(wave_top(sk)) - 15;
+      const float A = __builtin_amdgcn_ldexpf(sk, -E);  // in [0, 2^15)
+      const uint64_t vm = __builtin_amdgcn_ballot_w64(ok);
+      if (tid == 0) {
+        S.E = E;
+        S.valid[0] = (uint32_t)vm;
+        S.valid[1] = (uint32_t)(vm >> 32);
+      }
+      // A z 2^-17, against sum q 2^-7 (both below 2^15)
+      const Pieces u = pieces(ok ? A * (float)(int16_t)(par.x >> 16) * 0x1p-17f : 0.0f);
+      if ((lane >> 4) == grp)
+        S.z[lane] = make_uint4(pk_f16(u.h1, u.h1), pk_f16(u.h2, u.h1), pk_f16(u.h2, u.h3), 0);
+      const float mine = __shfl(A, 16 * grp + (lane >> 2));
+      const uint32_t a1 = pk_f16(mine, mine), a16 = pk_f16(mine * 0.0625f, mine * 0.0625f);
+      uint4* dst = reinterpret_cast<uint4*>(S.k + (16 * grp + (lane >> 2)) * KROW + (lane & 3) * (D / 2));
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) {
+        const uint32_t x = code[i], x8 = x >> 8;
+        dst[i] = make_uint4(pk_mul(x & 0x000F000Fu, a1), pk_mul(x & 0x00F000F0u, a16),
+                            pk_mul(x8 & 0x000F000Fu, a1), pk_mul(x8 & 0x00F000F0u, a16));
+      }
+    } else {
+      const float sv = ok ? fp16_bits_to_f32((uint16_t)par.y) : 0.0f;
+      const float z = ok ? (float)(int16_t)(par.y >> 16) : 0.0f;
+      const float top = wave_top(sv * (16.0f + fabsf(z)));
+      if (top > 0.0f) Fmax = max(Fmax, __builtin_amdgcn_frexp_expf(top) - 19);
+      if (tid == 256) S.F = Fmax;
+      const float A = __builtin_amdgcn_ldexpf(sv, -Fmax);  // A (16 + |z|) < 2^19
+      const uint32_t ab = pk_f16(A, -A * z * 0x1p-9f);
+      const int wd = lane % NV, qd = lane / NV % 4;
+      uint32_t s4[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s4[i] = __shfl(ab, 16 * grp + 4 * qd + i);
+      uint32_t o[8][2];
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        const uint32_t a1 = __builtin_amdgcn_perm(s4[2 * p + 1], s4[2 * p], 0x05040100u);
+        const uint32_t b1 = __builtin_amdgcn_perm(s4[2 * p + 1], s4[2 * p], 0x07060302u);
+        const uint32_t a16 = pk_mul(a1, 0x2C002C00u);  // / 16
+        const uint32_t x0 = __builtin_amdgcn_perm(code[2 * p + 1], code[2 * p], 0x05040100u);
+        const uint32_t x1 = __builtin_amdgcn_perm(code[2 * p + 1], code[2 * p], 0x07060302u);
+        const uint32_t x[4] = {x0, x0 >> 8, x1, x1 >> 8};
+#pragma unroll
+        for (int m = 0; m < 8; ++m)  // codes as subnormals, times 2^15, then A c 2^-9 - A z 2^-9
+          o[m][p] = pk_fma(pk_mul(x[m >> 1] & (m & 1 ? 0x00F000F0u : 0x000F000Fu), 0x78007800u),
+                           m & 1 ? a16 : a1, b1);
+      }
+      if (lane < 4 * NV) {
+        uint8_t* dst = S.v + wd * VROW + 2 * (16 * grp + 8 * (qd & 1) + 4 * (qd >> 1));
+#pragma unroll
+        for (int m = 0; m < 8; ++m)
+          *reinterpret_cast<uint2*>(dst + m * NV * VROW) = make_uint2(o[m][0], o[m][1]);
+      }
+    }
+  };
+  const bool any = kb0 < kb1;
+  if (any) {
+    load_ids();
+    load(kb0);
+  }
+
+  // ---- queries: channels D / 2 h .. of the row, rotated, scaled by a power of two into fp16
+  uint32_t qb[NS][4], zb[4] = {0, 0, 0, 0};
+  float qscale;
+  {
+    float x[D / 2];
+    const uint4* src = reinterpret_cast<const uint4*>(a.q + (int64_t)(w.s.q0 + tok) * a.ldq +
+                                                      (int64_t)hq * D + D / 2 * h);
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      const uint4 v = src[i];
+      const uint32_t y[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        x[8 * i + 2 * k] = bf16_lo(y[k]);
+        x[8 * i + 2 * k + 1] = bf16_hi(y[k]);
+      }
+    }
+    if (a.k_had) {
+#pragma unroll
+      for (int s = 1; s < D / 2; s <<= 1)
+#pragma unroll
+        for (int i = 0; i < D / 2; ++i)
+          if (!(i & s)) {
+            const float p = x[i], q = x[i + s];
+            x[i] = p + q;
+            x[i + s] = p - q;
+          }
+#pragma unroll
+      for (int i = 0; i < D / 2; ++i) {
+        const float p = __shfl_xor(x[i], 32);
+        x[i] = hadamard_norm<D>() * (h ? p - x[i] : x[i] + p);
+      }
+    }
+    float qm = 0.0f;
+#pragma unroll
+    for (int i = 0; i < D / 2; ++i) qm = fmaxf(qm, fabsf(x[i]));
+    qm = fmaxf(qm, __shfl_xor(qm, 32));
+    const int e15 = 15 - __builtin_amdgcn_frexp_expf(qm);
+    qscale = __builtin_amdgcn_ldexpf(a.sm_scale * LOG2E, 24 - e15);
+    float sum = 0.0f;
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const h2_t p = {(_Float16)__builtin_amdgcn_ldexpf(x[8 * s + k], e15),
+                        (_Float16)__builtin_amdgcn_ldexpf(x[8 * s + k + 4], e15)};
+        sum += (float)p.x + (float)p.y;
+        qb[s][k] = __builtin_bit_cast(uint32_t, p);
+      }
+    sum += __shfl_xor(sum, 32);
+    if (!h) {
+      const Pieces v = pieces(sum * -0x1p-7f);
+      zb[0] = pk_f16(v.h1, v.h2);
+      zb[1] = pk_f16(v.h1, v.h3);
+      zb[2] = pk_f16(v.h2, v.h1);
+    }
+  }
+
+  f16_t o[ND];
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
+  float m = LOWEST, l = 0.0f;
+  int F = -200;
+
+  if (any) store(st[0]);
   __syncthreads();
-  if (a.k_had) {
-    float y[E];
-    for (int e = 0; e < E; ++e) {
-      y[e] = 0.0f;
-      const int d = e * 64 + lane;
-      for (int k = 0; k < D; ++k) y[e] += (__builtin_popcount(k & d) & 1) ? -s_q[k] : s_q[k];
-    }
-    __syncthreads();
-    for (int e = 0; e < E; ++e) s_q[e * 64 + lane] = y[e] * hadamard_norm<D>();
-    __syncthreads();
-  }
-  const float NEG = -__builtin_inff();
-  float mx = NEG, l = 0.0f, o[E] = {};
-  for (int64_t j0 = 0; j0 < seen; j0 += 64) {
-    const int64_t j = j0 + lane;
-    float s = NEG;
-    int64_t r = -1;
-    if (j < seen) {
-      const int page = a.page_table[(int64_t)b * a.max_pages + (j >> c.log2p)];
-      if (page >= 0 && page < c.pages) {
-        r = c.row(page, hk, (int)(j & ((1 << c.log2p) - 1)));
-        const int z = c.par[4 * r + 1];
-        float dot = 0.0f;
-        for (int w = 0; w < D / 8; ++w) {
-          const uint32_t u = reinterpret_cast<const uint32_t*>(c.kc + r * (D / 2))[w];
-          for (int k = 0; k < 8; ++k)
-            dot = __builtin_fmaf(s_q[8 * w + k], (float)((int)((u >> (4 * k)) & 15u) - z), dot);
+  for (int kb = kb0; kb < kb1; ++kb) {
+    if (kb + 1 < kb1) load(kb + 1);
+    const Stage<D>& S = st[(kb - kb0) & 1];
+    if (live && kb * KB <= pmax) {
+      const float scl = __builtin_amdgcn_ldexpf(qscale, __builtin_amdgcn_readfirstlane(S.E));
+      const uint32_t valid[2] = {(uint32_t)__builtin_amdgcn_readfirstlane(S.valid[0]),
+                                 (uint32_t)__builtin_amdgcn_readfirstlane(S.valid[1])};
+      const int Fb = __builtin_amdgcn_readfirstlane(S.F);
+      if (Fb != F) {
+        const float f = __builtin_amdgcn_ldexpf(1.0f, max(F - Fb, -150));
+#pragma unroll
+        for (int d = 0; d < ND; ++d) o[d] *= f;
+        F = Fb;
+      }
+      f16_t s[2];
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[tt][r] = 0.0f;
+        s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+            __builtin_bit_cast(h8_t, S.z[32 * tt + ql]),
+            __builtin_bit_cast(h8_t, make_uint4(zb[0], zb[1], zb[2], zb[3])), s[tt], 0, 0, 0);
+#pragma unroll
+        for (int k = 0; k < NS; ++k) {
+          const uint4 kk = *reinterpret_cast<const uint4*>(S.k + (32 * tt + ql) * KROW + D * h + 16 * k);
+          s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+              __builtin_bit_cast(h8_t, kk),
+              __builtin_bit_cast(h8_t, make_uint4(qb[k][0], qb[k][1], qb[k][2], qb[k][3])), s[tt], 0, 0, 0);
         }
-        s = a.sm_scale * LOG2E * fp16_bits_to_f32((uint16_t)c.par[4 * r]) * dot;
+      }
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        // ---- one tile of 32 positions: mask, reference maximum, weights, value product
+        const int k0 = kb * KB + 32 * tt;
+        if (k0 + 31 > pmin || valid[tt] != 0xFFFFFFFFu) {
+          const uint32_t vm = valid[tt] >> (4 * h);
+          const int lim = pos - k0 - 4 * h;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int j = 8 * (r >> 2) + (r & 3);
+            if (j > lim || !((vm >> j) & 1)) s[tt][r] = -__builtin_inff();
+          }
+        }
+        float top = s[tt][0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) top = fmaxf(top, s[tt][r]);
+        if (__builtin_amdgcn_ballot_w64(__builtin_fmaf(top, scl, -m) > TOP)) {
+          top = fmaxf(top, __shfl_xor(top, 32));
+          const float mn = fmaxf(m, __builtin_fmaf(top, scl, -MID));
+          const float f = __builtin_amdgcn_exp2f(m - mn);
+          m = mn;
+          l *= f;
+#pragma unroll
+          for (int d = 0; d < ND; ++d) o[d] *= f;
+        }
+        uint32_t wb[2][4];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float x0 = __builtin_fmaf(s[tt][8 * k + 2 * j], scl, -m);
+            const float x1 = __builtin_fmaf(s[tt][8 * k + 2 * j + 1], scl, -m);
+            const h2_t p = {(_Float16)__builtin_amdgcn_exp2f(x0), (_Float16)__builtin_amdgcn_exp2f(x1)};
+            l = __builtin_amdgcn_fdot2(p, h2_t{(_Float16)1.0f, (_Float16)1.0f}, l, false);
+            wb[k][j] = __builtin_bit_cast(uint32_t, p);
+          }
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int d = 0; d < ND; ++d) {
+            const uint4 vv = *reinterpret_cast<const uint4*>(S.v + (32 * d + ql) * VROW +
+                                                             2 * (16 * (2 * tt + k) + 8 * h));
+            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                __builtin_bit_cast(h8_t, vv),
+                __builtin_bit_cast(h8_t, make_uint4(wb[k][0], wb[k][1], wb[k][2], wb[k][3])), o[d], 0, 0, 0);
+          }
       }
     }
-    float bm = s;
-    for (int off = 32; off >= 1; off >>= 1) bm = fmaxf(bm, __shfl_xor(bm, off));
-    if (bm == NEG) continue;
-    const float mn = fmaxf(mx, bm);
-    const float f = __builtin_amdgcn_exp2f(mx - mn);
-    const float p = __builtin_amdgcn_exp2f(s - mn);
-    mx = mn;
-    l = l * f + p;  // this lane's positions
-    s_p[lane] = p;
-    s_row[lane] = r;
-    __syncthreads();
-    for (int e = 0; e < E; ++e) o[e] *= f;
-    for (int k = 0; k < 64; ++k) {
-      const int64_t rk = s_row[k];
-      if (rk < 0) continue;
-      const float w = s_p[k] * fp16_bits_to_f32((uint16_t)c.par[4 * rk + 2]);
-      const int z = c.par[4 * rk + 3];
-      for (int e = 0; e < E; ++e) {
-        const int d = e * 64 + lane;
-        const int code = (c.vc[rk * (D / 2) + d / 2] >> (4 * (d & 1))) & 15;
-        o[e] = __builtin_fmaf(w, (float)(code - z), o[e]);
-      }
-    }
+    if (kb + 1 < kb1) store(st[(kb + 1 - kb0) & 1]);
     __syncthreads();
   }
-  for (int off = 32; off >= 1; off >>= 1) l += __shfl_xor(l, off);
-  for (int e = 0; e < E; ++e) o[e] = l > 0.0f ? o[e] / l : 0.0f;
-  if (a.v_had) {
-    __syncthreads();
-    for (int e = 0; e < E; ++e) s_q[e * 64 + lane] = o[e];
-    __syncthreads();
-    for (int e = 0; e < E; ++e) {
-      const int d = e * 64 + lane;
-      float y = 0.0f;
-      for (int k = 0; k < D; ++k) y += (__builtin_popcount(k & d) & 1) ? -s_q[k] : s_q[k];
-      o[e] = y * hadamard_norm<D>();
+  if (!live) return;
+  l += __shfl_xor(l, 32);
+
+  // ---- channels: o[d][r] is channel 8 word + nibble of V^T's row 32 d + 8 (r / 4) + 4 h + r % 4
+  // = nibble * D / 8 + word
+  const bool mine = wrow + ql <= last;
+  const float back = __builtin_amdgcn_ldexpf(1.0f, F + 9);  // (0 where nothing was met)
+  auto word = [&](int j, float* y) {  // this lane's j-th code word, j < D / 16
+#pragma unroll
+    for (int n = 0; n < 8; ++n)
+      y[n] = D == 128 ? o[n >> 1][8 * (n & 1) + 4 * (j >> 2) + (j & 3)] : o[n >> 2][4 * (n & 3) + j];
+  };
+  if (ns > 1) {
+    if (!mine) return;
+    float* dst = rec + (int64_t)((w.index * c.Hkv + hk) * splits + split) * ROWS * (D + 2);
+    const int i = 32 * wave + ql;
+    if (!h) *reinterpret_cast<float2*>(dst + 2 * i) = make_float2(m, l);
+    dst += 2 * ROWS + i * D;
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) {
+      float y[8];
+      word(j, y);
+      float4* p = reinterpret_cast<float4*>(dst + 8 * (D == 128 ? 8 * (j >> 2) + 4 * h + (j & 3) : 4 * h + j));
+      p[0] = make_float4(y[0] * back, y[1] * back, y[2] * back, y[3] * back);
+      p[1] = make_float4(y[4] * back, y[5] * back, y[6] * back, y[7] * back);
+    }
+    return;
+  }
+  const float f = l > 0.0f ? back / l : 0.0f;
+#pragma unroll
+  for (int d = 0; d < ND; ++d) o[d] *= f;
+  if (a.v_had) {  // every channel bit is a bit of d, r or h
+#pragma unroll
+    for (int s = 1; s < D / 2; s <<= 1)
+#pragma unroll
+      for (int i = 0; i < D / 2; ++i)
+        if (!(i & s)) {
+          const float p = o[i >> 4][i & 15], q = o[(i + s) >> 4][(i + s) & 15];
+          o[i >> 4][i & 15] = p + q;
+          o[(i + s) >> 4][(i + s) & 15] = p - q;
+        }
+#pragma unroll
+    for (int i = 0; i < D / 2; ++i) {
+      const float x = o[i >> 4][i & 15], p = __shfl_xor(x, 32);
+      o[i >> 4][i & 15] = hadamard_norm<D>() * (h ? p - x : x + p);
     }
   }
-  uint16_t* out = a.out + (int64_t)m * a.ldo + (int64_t)hq * D;
-  for (int e = 0; e < E; ++e) out[e * 64 + lane] = f32_to_bf16_rne(o[e]);
+  if (!mine) return;
+  uint16_t* dst = a.out + (int64_t)(w.s.q0 + tok) * a.ldo + (int64_t)hq * D;
+#pragma unroll
+  for (int j = 0; j < D / 16; ++j) {
+    float y[8];
+    word(j, y);
+    *reinterpret_cast<uint4*>(dst + 8 * (D == 128 ? 8 * (j >> 2) + 4 * h + (j & 3) : 4 * h + j)) =
+        make_uint4(bf16x2_rne(y[0], y[1]), bf16x2_rne(y[2], y[3]), bf16x2_rne(y[4], y[5]),
+                   bf16x2_rne(y[6], y[7]));
+  }
+}
+
+// Joins the splits of a tile's rows, a wave per row.
+template <int D>
+__global__ __launch_bounds__(256) void kv_attention_paged_tile_join_kernel(
+    PagedAttentionArgs a, int Hkv, int splits, const TileJoint* __restrict__ joints,
+    const float* __restrict__ rec) {
+  const int lane = (int)__builtin_amdgcn_workitem_id_x() & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((int)__builtin_amdgcn_workitem_id_x() >> 6);
+  const int id = (int)__builtin_amdgcn_workgroup_id_x();
+  const int i = 4 * (id % (ROWS / 4)) + wave, hk = id / (ROWS / 4) % Hkv, t = id / (ROWS / 4) / Hkv;
+  const TileJoint j = joints[t];
+  if (i >= j.rows || j.nsplit <= 1) return;
+  const int64_t size = ROWS * (D + 2);
+  const float* src = rec + (int64_t)(t * Hkv + hk) * splits * size;
+  float2 ml = make_float2(LOWEST, 0.0f);  // splits <= 64
+  if (lane < j.nsplit) ml = *reinterpret_cast<const float2*>(src + lane * size + 2 * i);
+  const float top = wave_max(ml.x);
+  const float f = __builtin_amdgcn_exp2f(ml.x - top);
+  const float l = wave_sum(f * ml.y);
+  float o[D / 64] = {};
+  src += 2 * ROWS + i * D + lane * (D / 64);
+  for (int k = 0; k < j.nsplit; ++k) {
+    const float fk = __shfl(f, k);
+#pragma unroll
+    for (int e = 0; e < D / 64; ++e) o[e] = __builtin_fmaf(fk, src[k * size + e], o[e]);
+  }
+  const int G = a.Hq / Hkv, row = j.row0 + i;
+  store_row<D>(a, j.q0 + row / G, hk * G + row % G, o, l, lane);
 }
 
 }  // namespace
 
 namespace {
 
-// How the few-row kernel is launched: the rows it takes, its row tiles, and its units.
-struct Few {
-  int rows, tiles, target, units, max_chunks;
-  bool join;
+// How a call is launched: the rows that the few-row kernel takes, its row tiles and units; the
+// tiles of the other kernel and over how many workgroups the keys of each are split.
+struct Shape {
+  bool few, many, few_join;
+  int few_rows, row_tiles, target, units, max_chunks;
+  int64_t tiles;
+  int splits;
 };
-Few few_shape(int64_t B, int64_t Hq, int64_t Hkv, int64_t max_new, int64_t cap) {
+Shape attention_shape(int64_t M, int64_t B, int64_t Hq, int64_t Hkv, int64_t max_new, int64_t cap) {
   const int64_t G = Hq / Hkv, most = max_new * G;
-  Few f;
-  f.tiles = most <= 16 ? 1 : most <= 32 ? 2 : most <= 64 ? 4 : 1;
-  f.rows = (int)(most <= 64 ? most : 16);
+  Shape f = {};
+  f.many = most > 64;
+  f.few = !f.many || B > 1;  // a single sequence of many rows: one launch
+  f.row_tiles = f.many || most <= 16 ? 1 : most <= 32 ? 2 : 4;
+  f.few_rows = f.few ? (int)(f.many ? 16 : most) : 0;
   f.target = 1024;
   f.max_chunks = 256;
-  f.join = cap > CHUNK_MIN;
-  f.units = (int)(f.join ? f.target + B * Hkv : B * Hkv);
+  f.few_join = f.few && cap > CHUNK_MIN;
+  f.units = (int)((f.few_join ? f.target : 0) + B * Hkv);
+  f.splits = 1;
+  if (f.many) {
+    // (a sequence adds at most one tile that is not full)
+    f.tiles = M * G / ROWS + (B < M ? B : M);
+    const int64_t wgs = f.tiles * Hkv;
+    // one workgroup per CU: the fewest splits that keep nine in ten of 256 CUs busy
+    for (int s = 1; s <= 64 && wgs * s <= 768; ++s) {
+      f.splits = s;
+      const int64_t rounds = (wgs * s + 255) / 256;
+      if (10 * wgs * s >= 9 * 256 * rounds) break;
+    }
+  }
   return f;
+}
+int64_t few_floats(const Shape& f, int64_t B, int D) {
+  return f.few_join ? 4 * B + (int64_t)f.units * f.few_rows * (D + 2) : 0;
+}
+int64_t tile_floats(const Shape& f, int64_t Hkv, int D) {
+  return f.splits > 1 ? 4 * f.tiles + f.tiles * Hkv * f.splits * ROWS * (D + 2) : 0;
 }
 
 }  // namespace
 
 int64_t kv_attention_paged_workspace_floats(int64_t M, int64_t B, int64_t Hq, int64_t Hkv,
                                             int head_dim, int64_t max_new) {
-  const Few f = few_shape(B, Hq, Hkv, max_new, int64_t(1) << 30);
-  return 4 * B + (int64_t)f.units * f.rows * (head_dim + 2);
+  const Shape f = attention_shape(M, B, Hq, Hkv, max_new, int64_t(1) << 30);
+  return (few_floats(f, B, head_dim) + 3) / 4 * 4 + tile_floats(f, Hkv, head_dim);
 }
 
 hipError_t launch_kv_attention_paged(const PagedAttentionArgs& a, const PagedCache& c, int head_dim,
                                      float* workspace, hipStream_t stream) {
-  const Few f = few_shape(a.B, a.Hq, c.Hkv, a.max_new, (int64_t)a.max_pages << c.log2p);
-  Joint* joints = f.join ? reinterpret_cast<Joint*>(workspace) : nullptr;
-  float* rec = workspace + 4 * (int64_t)a.B;
+  const Shape f = attention_shape(a.M, a.B, a.Hq, c.Hkv, a.max_new, (int64_t)a.max_pages << c.log2p);
+  if (f.few) {
+    Joint* joints = f.few_join ? reinterpret_cast<Joint*>(workspace) : nullptr;
+    float* rec = workspace + 4 * (int64_t)a.B;
 #define OFFQ_FEW(D_, RT_)                                                                        \
   hipLaunchKernelGGL((kv_attention_paged_few_kernel<D_, RT_>), dim3((unsigned)f.units), dim3(256), \
-                     0, stream, a, c, f.rows, f.target, f.max_chunks, joints, rec)
-  if (head_dim == 128) {
-    if (f.tiles == 1) OFFQ_FEW(128, 1);
-    else if (f.tiles == 2) OFFQ_FEW(128, 2);
-    else OFFQ_FEW(128, 4);
-  } else {
-    if (f.tiles == 1) OFFQ_FEW(64, 1);
-    else if (f.tiles == 2) OFFQ_FEW(64, 2);
-    else OFFQ_FEW(64, 4);
-  }
+                     0, stream, a, c, f.few_rows, f.target, f.max_chunks, joints, rec)
+    if (head_dim == 128) {
+      if (f.row_tiles == 1) OFFQ_FEW(128, 1);
+      else if (f.row_tiles == 2) OFFQ_FEW(128, 2);
+      else OFFQ_FEW(128, 4);
+    } else {
+      if (f.row_tiles == 1) OFFQ_FEW(64, 1);
+      else if (f.row_tiles == 2) OFFQ_FEW(64, 2);
+      else OFFQ_FEW(64, 4);
+    }
 #undef OFFQ_FEW
-  if (f.join) {
-    const dim3 grid((unsigned)(f.rows * c.Hkv * a.B));
-    hipLaunchKernelGGL(head_dim == 128 ? kv_attention_paged_join_kernel<128> : kv_attention_paged_join_kernel<64>,
-                       grid, dim3(256), 0, stream, a, c.Hkv, f.rows, joints, rec, c.log2p, f.rows);
+    if (f.few_join)
+      hipLaunchKernelGGL(head_dim == 128 ? kv_attention_paged_join_kernel<128>
+                                         : kv_attention_paged_join_kernel<64>,
+                         dim3((unsigned)(f.few_rows * c.Hkv * a.B)), dim3(256), 0, stream, a, c.Hkv,
+                         f.few_rows, joints, rec, c.log2p, f.few_rows);
   }
-  if (a.max_new * (a.Hq / c.Hkv) > f.rows) {
-    const dim3 grid((unsigned)a.M, (unsigned)a.Hq);
-    hipLaunchKernelGGL(head_dim == 128 ? kv_attention_paged_kernel<128> : kv_attention_paged_kernel<64>,
-                       grid, dim3(64), 0, stream, a, c, f.rows);
+  if (f.many) {
+    float* base = workspace + (few_floats(f, a.B, head_dim) + 3) / 4 * 4;
+    TileJoint* joints = f.splits > 1 ? reinterpret_cast<TileJoint*>(base) : nullptr;
+    float* rec = base + 4 * f.tiles;
+    const dim3 grid((unsigned)(f.tiles * c.Hkv * f.splits));
+    hipLaunchKernelGGL(head_dim == 128 ? kv_attention_paged_tile_kernel<128>
+                                       : kv_attention_paged_tile_kernel<64>,
+                       grid, dim3(512), 0, stream, a, c, f.few_rows, f.splits, joints, rec);
+    if (f.splits > 1)
+      hipLaunchKernelGGL(head_dim == 128 ? kv_attention_paged_tile_join_kernel<128>
+                                         : kv_attention_paged_tile_join_kernel<64>,
+                         dim3((unsigned)(f.tiles * c.Hkv * (ROWS / 4))), dim3(256), 0, stream, a, c.Hkv,
+                         f.splits, joints, rec);
   }
   return hipGetLastError();
 }
