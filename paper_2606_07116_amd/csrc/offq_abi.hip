@@ -606,7 +606,8 @@ offq_status_t offq_kv_attention_paged(const uint16_t* q, int64_t ldq, int64_t M,
   if (ldq < Hq * head_dim || ldq % 8 || ldo < Hq * head_dim || ldo % 8)
     return fail(OFFQ_ERR_INVALID, "need ldq, ldo >= Hq head_dim, multiples of 8");
   if (!paged_attention_sizes(M, B, Hq, Hkv, head_dim, max_new) ||
-      max_pages > (int64_t(1) << 30) / page_size || num_pages > (int64_t(1) << 31) - 1 ||
+      max_pages > (int64_t(1) << 30) / page_size ||
+      B * Hkv * (max_pages * page_size / 128 + 1) >= (int64_t(1) << 31) || num_pages > (int64_t(1) << 31) - 1 ||
       ldq > (int64_t(1) << 40) || ldo > (int64_t(1) << 40))
     return fail(OFFQ_ERR_UNSUPPORTED, "sizes too large");
   if (M == 0 || B == 0 || max_new == 0) return ok();  // empty: pointers may be NULL

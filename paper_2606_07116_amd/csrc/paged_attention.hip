@@ -54,8 +54,8 @@ __device__ __forceinline__ Seq sequence(const PagedAttentionArgs& a, int log2p, 
 // ---------------------------------------------------------------------------
 // Few rows: sequences of up to 16 RT query rows (new tokens x heads of a group).  What bounds
 // them is the cache's bytes, so the keys of all such sequences are cut into chunks of one length,
-// chosen on the device so that about `target` workgroups get one each whatever the lengths are;
-// a chunk's four waves take a quarter each, and a second kernel joins a row's chunks.
+// chosen on the device so that the resident workgroups get one each whatever the lengths are; a
+// chunk's four waves take a quarter each, and a second kernel joins a row's chunks.
 //
 // A wave takes 32 positions at a time, two groups of 16 (a group lies in one page), straight from
 // memory into the operands of 16x16x32 fp16 matrix products, the next block's loads in flight:
@@ -78,39 +78,61 @@ struct Chunking {
   Seq s;
 };
 
-// The chunk length, and what unit `unit` is.  Every wave works it out for itself, 64 sequences
-// at a time.
+// Sum and maximum over a wave, the same in every lane.
+__device__ __forceinline__ int wave_add(int v) {
+  v += __builtin_amdgcn_mov_dpp(v, 0x128, 0xf, 0xf, true);  // rotations within rows of 16 lanes
+  v += __builtin_amdgcn_mov_dpp(v, 0x124, 0xf, 0xf, true);
+  v += __builtin_amdgcn_mov_dpp(v, 0x122, 0xf, 0xf, true);
+  v += __builtin_amdgcn_mov_dpp(v, 0x121, 0xf, 0xf, true);
+  return (__builtin_amdgcn_readlane(v, 0) + __builtin_amdgcn_readlane(v, 16)) +
+         (__builtin_amdgcn_readlane(v, 32) + __builtin_amdgcn_readlane(v, 48));
+}
+
+// The chunk length, and what unit `unit` is.  `slots` workgroups are resident at once.  One round
+// of units costs its longest chunk, so the shortest length whose units fit the slots is tried
+// first; where it is far above the mean (a few long sequences among many), chunks of half the
+// mean in several rounds.  The cost of a unit besides its positions is that of about 400 (6 us).
+// Every wave works it out for itself, 64 sequences at a time.
 __device__ __forceinline__ Chunking find_chunk(const PagedAttentionArgs& a, int log2p, int Hkv,
-                                               int few_rows, int target, int max_chunks, int unit) {
+                                               int few_rows, int slots, int unit) {
   const int lane = (int)__builtin_amdgcn_workitem_id_x() & 63;
   const int G = a.Hq / Hkv;
-  float total = 0.0f;
-  int longest = 0;
   Seq s{};
   auto load = [&](int b) {
     s = Seq{};
     if (b < a.B) s = sequence(a, log2p, G, b);
     if (s.rows > few_rows) s.rows = 0;
   };
+  auto chunks = [&](int len) { return s.rows ? max(1, (s.keys + len - 1) / len) : 0; };
+  auto units = [&](int len) {
+    int n = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+      if (a.B > 64) load(b0 + lane);
+      n += chunks(len);
+    }
+    return (int64_t)Hkv * wave_add(n);
+  };
+  int64_t total = 0;  // in blocks of 128
   for (int b0 = 0; b0 < a.B; b0 += 64) {
     load(b0 + lane);
-    if (s.rows) {
-      total += (float)s.keys;
-      longest = max(longest, s.keys);
-    }
+    total += wave_add(s.rows ? (s.keys + 127) >> 7 : 0);
   }
-  total = wave_sum(total);
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) longest = max(longest, __shfl_xor(longest, o));
+  const int mean = (int)min((total * Hkv * 128 + slots - 1) / slots, (int64_t)1 << 30);
+  auto round_up = [](int64_t v) { return (int)max((int64_t)CHUNK_MIN, (v + 127) & ~(int64_t)127); };
+  const int several = round_up((mean + 1) / 2);  // at most 2 slots + a unit per sequence and head
   Chunking c{};
-  // (a rounding of the fp32 sum only shifts the chunk length, the same for every unit)
-  const float want = fminf(fmaxf(total * (float)Hkv / (float)target, (float)longest / (float)max_chunks),
-                           1073741824.0f);
-  c.len = max(CHUNK_MIN, ((int)want + 128) & ~127);
+  c.len = round_up(mean);
+  for (int64_t n = units(c.len); n > slots; n = units(c.len)) {
+    if (c.len > mean + several / 2 + 400) {
+      c.len = several;
+      break;
+    }
+    c.len = round_up(c.len + c.len / 16 + 1);
+  }
   int base = 0;
   for (int b0 = 0; b0 < a.B; b0 += 64) {
     if (a.B > 64) load(b0 + lane);
-    const int nc = s.rows ? max(1, (s.keys + c.len - 1) / c.len) : 0;
+    const int nc = chunks(c.len);
     int incl = nc;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -186,9 +208,9 @@ __device__ __forceinline__ void store_row(const PagedAttentionArgs& a, int row, 
 }
 
 template <int D, int RT>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RT == 1 ? 3 : 2))) void
-kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, int target,
-                              int max_chunks, Joint* __restrict__ joints, float* __restrict__ rec) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void
+kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, int slots,
+                              Joint* __restrict__ joints, float* __restrict__ rec) {
   constexpr int NW = D / 32;  // key code words of a lane
   constexpr int NM = D / 16;  // products of a value block: 16 columns of NM channels each
   constexpr int OROW = D + 4;
@@ -196,7 +218,8 @@ kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, 
     _Float16 q[16 * RT][D + 8];  // the queries in operand order
     float o[4][16][OROW];        // a row tile's outputs, one per wave
   } u;
-  __shared__ float4 s_par[4][32];  // per wave and position: score slope, score offset / sum q, sv, zv
+  // per wave and position: (score slope, score offset / sum q), (sv, zv)
+  __shared__ alignas(16) float2 s_kp[4][32], s_vp[4][32];
   __shared__ float s_qsum[16 * RT], s_qmax[4];
   __shared__ float s_m[4][16 * RT], s_l[4][16 * RT], s_z[4][16 * RT], s_scale[4];
 
@@ -205,7 +228,7 @@ kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, 
   const int pr = lane & 15, kq = lane >> 4;
   const int unit = (int)__builtin_amdgcn_workgroup_id_x();
   const int G = a.Hq / c.Hkv;
-  const Chunking w = find_chunk(a, c.log2p, c.Hkv, few_rows, target, max_chunks, unit);
+  const Chunking w = find_chunk(a, c.log2p, c.Hkv, few_rows, slots, unit);
   if (!w.found) return;
   const int rows = w.s.rows, hk = w.head;
   if (joints && w.chunk == 0 && hk == 0 && tid == 0)
@@ -350,7 +373,10 @@ kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, 
       v_lim = lim;
       v_mul = 128.0f / lim;
     }
-    if (lane < 32) s_par[wave][lane] = make_float4(sk, -sk * zk, sv * v_mul, zv);
+    if (lane < 32) {
+      s_kp[wave][lane] = make_float2(sk, -sk * zk);
+      s_vp[wave][lane] = make_float2(sv * v_mul, zv);
+    }
     __builtin_amdgcn_wave_barrier();
     f4_t d[RT][2];
 #pragma unroll
@@ -367,21 +393,28 @@ kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, 
                                                            d[t][g], 0, 0, 0);
       }
     }
-    float4 p4[2][4];
+    // this lane's positions, two to a 16-byte read
+    float4 kp[4], vp[4];
 #pragma unroll
-    for (int g = 0; g < 2; ++g)
+    for (int i = 0; i < 4; ++i)
+      kp[i] = *reinterpret_cast<const float4*>(&s_kp[wave][16 * (i >> 1) + 4 * kq + 2 * (i & 1)]);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) p4[g][r] = s_par[wave][16 * g + 4 * kq + r];
-    __builtin_amdgcn_wave_barrier();
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        f4_t& x = d[t][i >> 1];
+        const int r = 2 * (i & 1);
+        x[r] = __builtin_fmaf(kp[i].x, x[r], kp[i].y * qs[t]);
+        x[r + 1] = __builtin_fmaf(kp[i].z, x[r + 1], kp[i].w * qs[t]);
+      }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      vp[i] = *reinterpret_cast<const float4*>(&s_vp[wave][16 * (i >> 1) + 4 * kq + 2 * (i & 1)]);
     uint32_t wb[RT][4];
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-      float sc[2][4], top = -__builtin_inff();
-#pragma unroll
-      for (int g = 0; g < 2; ++g)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          sc[g][r] = __builtin_fmaf(p4[g][r].x, d[t][g][r], p4[g][r].y * qs[t]);
+      f4_t (&sc)[2] = d[t];
+      float top = -__builtin_inff();
       if (vm != 0xFFFFFFFFu || k0 + 31 > w.s.pos0) {
 #pragma unroll
         for (int g = 0; g < 2; ++g)
@@ -411,25 +444,18 @@ kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, 
           for (int k = 0; k < NM; ++k) o[t][k][r] *= fr;
         }
       }
-      float wf[2][4];
 #pragma unroll
-      for (int g = 0; g < 2; ++g)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float p = __builtin_amdgcn_exp2f(sc[g][r] - m[t]);
-          l[t] += p;
-          wf[g][r] = p * p4[g][r].z;
-        }
-#pragma unroll
-      for (int g = 0; g < 2; ++g)
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const h2_t h = {(_Float16)wf[g][2 * r], (_Float16)wf[g][2 * r + 1]};
-          wb[t][2 * g + r] = __builtin_bit_cast(uint32_t, h);
-          zs[t] = __builtin_fmaf((float)h.x, p4[g][2 * r].w, zs[t]);
-          zs[t] = __builtin_fmaf((float)h.y, p4[g][2 * r + 1].w, zs[t]);
-        }
+      for (int i = 0; i < 4; ++i) {
+        const float p0 = __builtin_amdgcn_exp2f(sc[i >> 1][2 * (i & 1)] - m[t]);
+        const float p1 = __builtin_amdgcn_exp2f(sc[i >> 1][2 * (i & 1) + 1] - m[t]);
+        l[t] += p0 + p1;
+        const h2_t h = {(_Float16)(p0 * vp[i].x), (_Float16)(p1 * vp[i].z)};
+        wb[t][i] = __builtin_bit_cast(uint32_t, h);
+        zs[t] = __builtin_fmaf((float)h.x, vp[i].y, zs[t]);
+        zs[t] = __builtin_fmaf((float)h.y, vp[i].w, zs[t]);
+      }
     }
+    __builtin_amdgcn_wave_barrier();
     // ---- values: operand slots 4 kq .. 4 kq + 3 of both groups, two positions a word
     uint32_t xs[4][NM / 2];
 #pragma unroll
@@ -1122,7 +1148,7 @@ namespace {
 // tiles of the other kernel and over how many workgroups the keys of each are split.
 struct Shape {
   bool few, many, few_join;
-  int few_rows, row_tiles, target, units, max_chunks;
+  int few_rows, row_tiles, slots, units;
   int64_t tiles;
   int splits;
 };
@@ -1133,10 +1159,9 @@ Shape attention_shape(int64_t M, int64_t B, int64_t Hq, int64_t Hkv, int64_t max
   f.few = !f.many || B > 1;  // a single sequence of many rows: one launch
   f.row_tiles = f.many || most <= 16 ? 1 : most <= 32 ? 2 : 4;
   f.few_rows = f.few ? (int)(f.many ? 16 : most) : 0;
-  f.target = 1024;
-  f.max_chunks = 256;
+  f.slots = 512;  // two workgroups a CU
   f.few_join = f.few && cap > CHUNK_MIN;
-  f.units = (int)((f.few_join ? f.target : 0) + B * Hkv);
+  f.units = (int)((f.few_join ? 2 * f.slots : 0) + B * Hkv);
   f.splits = 1;
   if (f.many) {
     // (a sequence adds at most one tile that is not full)
@@ -1174,7 +1199,7 @@ hipError_t launch_kv_attention_paged(const PagedAttentionArgs& a, const PagedCac
     float* rec = workspace + 4 * (int64_t)a.B;
 #define OFFQ_FEW(D_, RT_)                                                                        \
   hipLaunchKernelGGL((kv_attention_paged_few_kernel<D_, RT_>), dim3((unsigned)f.units), dim3(256), \
-                     0, stream, a, c, f.few_rows, f.target, f.max_chunks, joints, rec)
+                     0, stream, a, c, f.few_rows, f.slots, joints, rec)
     if (head_dim == 128) {
       if (f.row_tiles == 1) OFFQ_FEW(128, 1);
       else if (f.row_tiles == 2) OFFQ_FEW(128, 2);
