@@ -34,6 +34,9 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v;
 }
 
+// (a uniform value that went through the vector units, a division for instance)
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
 // What a sequence asks for, lengths made safe whatever the tables hold: `rows` query rows
 // (token, head of the group) of a key/value head, the first of them token q0 at position pos0,
 // and `keys` positions that the last of them sees.
@@ -117,7 +120,7 @@ __device__ __forceinline__ Chunking find_chunk(const PagedAttentionArgs& a, int 
     load(b0 + lane);
     total += wave_add(s.rows ? (s.keys + 127) >> 7 : 0);
   }
-  const int mean = (int)min((total * Hkv * 128 + slots - 1) / slots, (int64_t)1 << 30);
+  const int mean = uniform((int)min((total * Hkv * 128 + slots - 1) / slots, (int64_t)1 << 30));
   auto round_up = [](int64_t v) { return (int)max((int64_t)CHUNK_MIN, (v + 127) & ~(int64_t)127); };
   const int several = round_up((mean + 1) / 2);  // at most 2 slots + a unit per sequence and head
   Chunking c{};
@@ -147,7 +150,7 @@ __device__ __forceinline__ Chunking find_chunk(const PagedAttentionArgs& a, int 
       c.b = b0 + o;
       c.nchunk = __builtin_amdgcn_readlane(nc, o);
       c.unit0 = Hkv * __builtin_amdgcn_readlane(first, o);
-      c.head = (unit - c.unit0) / c.nchunk;
+      c.head = uniform((unit - c.unit0) / c.nchunk);
       c.chunk = unit - c.unit0 - c.head * c.nchunk;
       c.s.q0 = __builtin_amdgcn_readlane(s.q0, o);
       c.s.rows = __builtin_amdgcn_readlane(s.rows, o);
@@ -242,7 +245,10 @@ kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, 
   const int32_t* table = a.page_table + (int64_t)w.b * a.max_pages;
   auto load_ids = [&](int from) {
     const int key = from + 16 * lane;
-    return key < k_stop ? table[key >> c.log2p] : -1;
+    int id = key < k_stop ? table[key >> c.log2p] : -1;
+    // (waited for here, where it is rare: not after the branch, with all loads in flight)
+    asm volatile("" : "+v"(id));
+    return id;
   };
   int id0 = k_begin;
   int ids = load_ids(id0);
@@ -623,35 +629,50 @@ __global__ __launch_bounds__(256) void kv_attention_paged_join_kernel(
 // key the products bound it, so both run as 32x32x16 fp16 matrix products and everything that
 // can leave the score loop does:
 // * a block's codes become fp16 values once per workgroup, on their way to LDS: keys A c with
-//   A = sk 2^-E (a power of two per block), values A (c - z) with A = sv 2^-F (F follows the
-//   largest sv (16 + |z|) met), one rounding each (2^-11; a value's zero-point term another).  Per
-//   weight there is no scale, no zero-point and no slope left to apply;
+//   A = sk 2^-E, values A (c - z) with A = sv 2^-F, one rounding each (2^-11; a value's zero-point
+//   term another).  E and F are the workgroup's and follow the largest sk (8192 + |z|) and
+//   sv (16 + |z|) met, rarely; the query carries sm_scale log2(e) 2^E;
 // * the keys' zero-point term -z_j sum q, which can be far larger than the score, is a k-step of
 //   its own: A z_j and sum q as three fp16 pieces each, their six leading products;
+// * the score product starts from -m, the row's reference, so what it leaves are the exponents of
+//   the weights: per weight one exp2, half a conversion to fp16 and half a dot product for the
+//   sum.  That a reference has to move shows in the sum itself: infinite where a weight left the
+//   fp16 range, zero before the first position;
 // * S^T = K Q^T: a lane holds 16 positions of one query row per tile of 32, so maximum and sum
 //   stay in the lane, and the tile is in the operand layout of O^T = V^T P^T; V^T lies in LDS with
 //   the positions in the order of the accumulator and the channels as (nibble, code word), so
 //   that a lane ends with eight consecutive channels of each of its words;
-// * weights are 2^(s - m), m lagging so that they stay within [2^-24, 2^15] around 2^7; their sum
-//   is taken of the rounded ones.
+// * a moved reference puts the row's largest weight of that tile at 2^7: 2^9 below the range's
+//   end, and what lies 2^31 below it still counts.  The sum is taken of the rounded weights.
 // Longest tiles start first.  Where the tiles do not fill the CUs, the keys of a tile are split
 // over workgroups and the rows joined by a second kernel.
 constexpr int ROWS = 256;      // query rows of a tile
 constexpr int KB = 64;         // positions of a block
 constexpr int VROW = 2 * KB + 16;
-constexpr float TOP = 15.0f;   // a weight 2^x may rise to x = 15 before its row's reference moves,
-constexpr float MID = 7.0f;    // to put the largest at x = 7
+constexpr float MID = 7.0f;    // a reference that moves puts its row's largest weight at 2^MID
+constexpr float HUGE_SUM = 3e38f;
 
 typedef float f16_t __attribute__((ext_vector_type(16)));
 
 template <int D>
 struct alignas(16) Stage {
-  uint8_t k[KB * (2 * D + 16)];  // per position: A c, 8 fp16 per code word, in operand order
-  uint8_t v[D * VROW];           // per channel (nibble * D / 8 + word): A (c - z) of the 64 positions
-  uint4 z[KB];                   // per position: the pieces of A z
-  int E, F;
-  uint32_t valid[2];             // bit j: position j is seen (by rows past it)
+  uint8_t k[3][KB * (2 * D + 16)];  // per position: A c 2^-9, 8 fp16 per code word, in operand order
+  uint8_t v[2][D * VROW];           // per channel (nibble * D / 8 + word): A (c - z) 2^-9 of the 64 positions
+  struct Par {                      // what a block's codes are staged with
+    uint4 z[KB];                    // per position: the pieces of the keys' A z 2^-13
+    uint32_t a[KB];                 // the keys' A and A / 16
+    uint32_t ab[KB];                // the values' A and -A z 2^-9
+    int E, F;
+    uint32_t valid[2];              // bit j: position j is there
+  } par[4];
 };
+
+// Workgroup barrier for LDS traffic only: global loads in flight stay in flight.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
 
 __device__ __forceinline__ uint32_t pk_f16(float a, float b) {
   const h2_t h = {(_Float16)a, (_Float16)b};
@@ -759,13 +780,15 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
   constexpr int NS = D / 16;   // k-steps of the score product
   constexpr int ND = D / 32;   // tiles of output channels
   constexpr int NV = D / 8;    // code words of a row
-  __shared__ Stage<D> st[2];
+  __shared__ Stage<D> S;
+  __shared__ float s_qm[8];
   const int tid = (int)__builtin_amdgcn_workitem_id_x();
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int ql = lane & 31, h = lane >> 5;
   const int G = a.Hq / c.Hkv;
   const int id = (int)__builtin_amdgcn_workgroup_id_x();
-  const int split = id % splits, hk = id / splits % c.Hkv, t = id / splits / c.Hkv;
+  const int split = uniform(id % splits), hk = uniform(id / splits % c.Hkv);
+  const int t = uniform(id / splits / c.Hkv);
   const Tile w = find_tile(a, c.log2p, G, few_rows, t);
   if (!w.found) {
     if (joints && !split && !hk && !tid) joints[t] = TileJoint{0, 0, 0, 0};
@@ -774,138 +797,157 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
   const int row0 = w.i * ROWS;
   const int last = min(w.s.rows, row0 + ROWS) - 1;  // the tile's last row
   // the positions that its rows see, and this split's blocks of them
-  const int keys = (int)min((int64_t)max(w.s.pos0 + last / G + 1, 0), (int64_t)w.s.keys);
+  const int keys = uniform(min(max(w.s.pos0 + last / G + 1, 0), w.s.keys));
   const int nblk = (keys + KB - 1) / KB;
   const int ns = max(1, min(splits, nblk / 4));
   if (joints && !split && !hk && !tid) joints[w.index] = TileJoint{w.s.q0, row0, last + 1 - row0, ns};
   if (split >= ns) return;
-  const int kb0 = (int)((int64_t)nblk * split / ns), kb1 = (int)((int64_t)nblk * (split + 1) / ns);
+  const int kb0 = uniform((int)((int64_t)nblk * split / ns));
+  const int kb1 = uniform((int)((int64_t)nblk * (split + 1) / ns));
 
   // ---- this wave's rows
   const int wrow = row0 + 32 * wave;
-  const bool live = wrow <= last;
   const int row = min(wrow + ql, last);
   const int tok = row / G, hq = hk * G + row - tok * G;
   const int pos = w.s.pos0 + tok;
-  const int pmin = w.s.pos0 + wrow / G, pmax = w.s.pos0 + min(wrow + 31, last) / G;
+  const int pmin = uniform(w.s.pos0 + wrow / G);
 
-  // ---- staging: waves 0..3 16 positions of keys each, waves 4..7 of values
+  // ---- staging: eight positions a wave; a block's parameters are prepared by one wave, in turn
   const int32_t* table = a.page_table + (int64_t)w.b * a.max_pages;
-  const int grp = wave & 3;
-  const bool vwave = wave >= 4;
-  int id0 = kb0 * KB, ids = -1;  // lane i: the page of the 16 positions from id0 + 16 i on
-  auto load_ids = [&]() {
-    const int key = id0 + 16 * lane;
-    ids = key < keys ? table[key >> c.log2p] : -1;
+  const int pmask = (1 << c.log2p) - 1;
+  const int kkey = 8 * wave + (lane >> 3);                     // key staging: position, part lane % 8
+  const int vword = lane % NV, vpair = (lane / NV) & 3;        // value staging: word, two positions
+  const int vkey = 8 * wave + 2 * vpair;
+  struct Pages {  // lane i: the page of the 16 positions from id0 + 16 i on
+    int id0, ids;
+  } kpg, vpg;
+  auto find_pages = [&](Pages& p, int from) {
+    p.id0 = from;
+    const int key = from + 16 * lane;
+    p.ids = key < keys ? table[key >> c.log2p] : -1;
+    // (waited for here, where it is rare: not after the branch, with all loads in flight)
+    asm volatile("" : "+v"(p.ids));
   };
-  uint32_t code[4];
-  uint2 par;
-  bool ok;
-  int Fmax = -200;
-  auto load = [&](int kb) {
+  uint32_t kcode[2], vcode[2];
+  auto first_row = [&](Pages& p, int kb) {  // of the wave's eight positions
     const int k0 = kb * KB;
-    if (k0 - id0 >= 1024) {
-      id0 = k0;
-      load_ids();
-    }
-    const int gi = (k0 - id0) >> 4, off = k0 & ((1 << c.log2p) - 1);
-    const int mask = (1 << c.log2p) - 1;
-    // this wave's group of codes
-    int pg = __builtin_amdgcn_readlane(ids, gi + grp);
-    if (pg < 0 || pg >= c.pages) pg = 0;
-    const int64_t r = c.row(pg, hk, (off + 16 * grp) & mask);
-    if (!vwave) {
-      const uint8_t* p = c.kc + r * (D / 2) + (uint32_t)((lane >> 2) * (D / 2) + (lane & 3) * (D / 8));
-      if constexpr (D == 128) {
-        const uint4 x = *reinterpret_cast<const uint4*>(p);
-        code[0] = x.x;
-        code[1] = x.y;
-        code[2] = x.z;
-        code[3] = x.w;
-      } else {
-        const uint2 x = *reinterpret_cast<const uint2*>(p);
-        code[0] = x.x;
-        code[1] = x.y;
-      }
-    } else {
-      const uint8_t* p = c.vc + r * (D / 2) +
-                         (uint32_t)(4 * (lane / NV % 4) * (D / 2) + 4 * (lane % NV));
-#pragma unroll
-      for (int i = 0; i < 4; ++i) code[i] = *reinterpret_cast<const uint32_t*>(p + i * (D / 2));
-    }
-    // the parameters of position `lane` of the block
-    const int pl = __shfl(ids, gi + (lane >> 4));
-    ok = pl >= 0 && pl < c.pages && k0 + lane < keys;
-    par = *reinterpret_cast<const uint2*>(
-        c.par + 4 * c.row(ok ? pl : 0, hk, (off + (lane & 48)) & mask) + 4 * (lane & 15));
+    if (k0 - p.id0 >= 1024) find_pages(p, k0);
+    const int pg = __builtin_amdgcn_readlane(p.ids, ((k0 - p.id0) >> 4) + (wave >> 1));
+    return c.row((uint32_t)pg < (uint32_t)c.pages ? pg : 0, hk, (k0 + 8 * wave) & pmask);
   };
-  auto store = [&](Stage<D>& S) {
-    if (!vwave) {
-      const float sk = ok ? fp16_bits_to_f32((uint16_t)par.x) : 0.0f;
-      const int E = __builtin_amdgcn_frexp_expf(wave_top(sk)) - 15;
-      const float A = __builtin_amdgcn_ldexpf(sk, -E);  // in [0, 2^15)
-      const uint64_t vm = __builtin_amdgcn_ballot_w64(ok);
-      if (tid == 0) {
-        S.E = E;
-        S.valid[0] = (uint32_t)vm;
-        S.valid[1] = (uint32_t)(vm >> 32);
-      }
-      // A z 2^-17, against sum q 2^-7 (both below 2^15)
-      const Pieces u = pieces(ok ? A * (float)(int16_t)(par.x >> 16) * 0x1p-17f : 0.0f);
-      if ((lane >> 4) == grp)
-        S.z[lane] = make_uint4(pk_f16(u.h1, u.h1), pk_f16(u.h2, u.h1), pk_f16(u.h2, u.h3), 0);
-      const float mine = __shfl(A, 16 * grp + (lane >> 2));
-      const uint32_t a1 = pk_f16(mine, mine), a16 = pk_f16(mine * 0.0625f, mine * 0.0625f);
-      uint4* dst = reinterpret_cast<uint4*>(S.k + (16 * grp + (lane >> 2)) * KROW + (lane & 3) * (D / 2));
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i) {
-        const uint32_t x = code[i], x8 = x >> 8;
-        dst[i] = make_uint4(pk_mul(x & 0x000F000Fu, a1), pk_mul(x & 0x00F000F0u, a16),
-                            pk_mul(x8 & 0x000F000Fu, a1), pk_mul(x8 & 0x00F000F0u, a16));
-      }
+  auto load_k = [&](int kb) {
+    const uint8_t* src = c.kc + first_row(kpg, kb) * (D / 2);
+    const uint32_t at = (uint32_t)((lane >> 3) * (D / 2) + (lane & 7) * (D / 16));
+    if constexpr (D == 128) {
+      const uint2 y = *reinterpret_cast<const uint2*>(src + at);
+      kcode[0] = y.x;
+      kcode[1] = y.y;
     } else {
-      const float sv = ok ? fp16_bits_to_f32((uint16_t)par.y) : 0.0f;
-      const float z = ok ? (float)(int16_t)(par.y >> 16) : 0.0f;
-      const float top = wave_top(sv * (16.0f + fabsf(z)));
-      if (top > 0.0f) Fmax = max(Fmax, __builtin_amdgcn_frexp_expf(top) - 19);
-      if (tid == 256) S.F = Fmax;
-      const float A = __builtin_amdgcn_ldexpf(sv, -Fmax);  // A (16 + |z|) < 2^19
-      const uint32_t ab = pk_f16(A, -A * z * 0x1p-9f);
-      const int wd = lane % NV, qd = lane / NV % 4;
-      uint32_t s4[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) s4[i] = __shfl(ab, 16 * grp + 4 * qd + i);
-      uint32_t o[8][2];
-#pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        const uint32_t a1 = __builtin_amdgcn_perm(s4[2 * p + 1], s4[2 * p], 0x05040100u);
-        const uint32_t b1 = __builtin_amdgcn_perm(s4[2 * p + 1], s4[2 * p], 0x07060302u);
-        const uint32_t a16 = pk_mul(a1, 0x2C002C00u);  // / 16
-        const uint32_t x0 = __builtin_amdgcn_perm(code[2 * p + 1], code[2 * p], 0x05040100u);
-        const uint32_t x1 = __builtin_amdgcn_perm(code[2 * p + 1], code[2 * p], 0x07060302u);
-        const uint32_t x[4] = {x0, x0 >> 8, x1, x1 >> 8};
-#pragma unroll
-        for (int m = 0; m < 8; ++m)  // codes as subnormals, times 2^15, then A c 2^-9 - A z 2^-9
-          o[m][p] = pk_fma(pk_mul(x[m >> 1] & (m & 1 ? 0x00F000F0u : 0x000F000Fu), 0x78007800u),
-                           m & 1 ? a16 : a1, b1);
-      }
-      if (lane < 4 * NV) {
-        uint8_t* dst = S.v + wd * VROW + 2 * (16 * grp + 8 * (qd & 1) + 4 * (qd >> 1));
-#pragma unroll
-        for (int m = 0; m < 8; ++m)
-          *reinterpret_cast<uint2*>(dst + m * NV * VROW) = make_uint2(o[m][0], o[m][1]);
-      }
+      kcode[0] = *reinterpret_cast<const uint32_t*>(src + at);
     }
+  };
+  auto load_v = [&](int kb) {
+    const uint8_t* src = c.vc + first_row(vpg, kb) * (D / 2);
+    const uint32_t at = (uint32_t)(2 * vpair * (D / 2) + 4 * vword);
+    vcode[0] = *reinterpret_cast<const uint32_t*>(src + at);
+    vcode[1] = *reinterpret_cast<const uint32_t*>(src + at + D / 2);
+  };
+  auto store_k = [&](int kb, int slot) {
+    const h2_t aa = __builtin_bit_cast(h2_t, S.par[kb & 3].a[kkey]);
+    const uint32_t a1 = __builtin_bit_cast(uint32_t, h2_t{aa.x, aa.x});
+    const uint32_t a16 = __builtin_bit_cast(uint32_t, h2_t{aa.y, aa.y});
+    uint4* dst = reinterpret_cast<uint4*>(S.k[slot] + kkey * KROW + (lane & 7) * (D / 4));
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) {  // codes as subnormals, times 2^15, then A c 2^-9
+      const uint32_t y = kcode[i], y8 = y >> 8;
+      dst[i] = make_uint4(pk_mul(pk_mul(y & 0x000F000Fu, 0x78007800u), a1),
+                          pk_mul(pk_mul(y & 0x00F000F0u, 0x78007800u), a16),
+                          pk_mul(pk_mul(y8 & 0x000F000Fu, 0x78007800u), a1),
+                          pk_mul(pk_mul(y8 & 0x00F000F0u, 0x78007800u), a16));
+    }
+  };
+  auto store_v = [&](int kb, int slot) {
+    const uint2 s01 = *reinterpret_cast<const uint2*>(&S.par[kb & 3].ab[vkey]);
+    const uint32_t a1 = __builtin_amdgcn_perm(s01.y, s01.x, 0x05040100u);
+    const uint32_t b1 = __builtin_amdgcn_perm(s01.y, s01.x, 0x07060302u);
+    const uint32_t a16 = pk_mul(a1, 0x2C002C00u);  // / 16
+    const uint32_t x0 = __builtin_amdgcn_perm(vcode[1], vcode[0], 0x05040100u);
+    const uint32_t x1 = __builtin_amdgcn_perm(vcode[1], vcode[0], 0x07060302u);
+    const uint32_t y[4] = {x0, x0 >> 8, x1, x1 >> 8};
+    // position 16 a + 8 b + 4 h + i of the block stands at 16 a + 8 h + 4 b + i
+    uint8_t* dst = S.v[slot] + vword * VROW +
+                   2 * (16 * (wave >> 1) + 8 * (vpair >> 1) + 4 * (wave & 1) + 2 * (vpair & 1));
+    if (D == 128 || lane < 32) {
+#pragma unroll
+      for (int m = 0; m < 8; ++m)  // codes as subnormals, times 2^15, then A c 2^-9 - A z 2^-9
+        *reinterpret_cast<uint32_t*>(dst + m * NV * VROW) =
+            pk_fma(pk_mul(y[m >> 1] & (m & 1 ? 0x00F000F0u : 0x000F000Fu), 0x78007800u),
+                   m & 1 ? a16 : a1, b1);
+    }
+  };
+  // Parameters, lane = position: the page first, then (a turn later) the row's, then its place.
+  auto page_of = [&](int kb) {
+    const int key = kb * KB + lane;
+    return key < keys ? table[key >> c.log2p] : -1;
+  };
+  auto params = [&](int kb, int page) {
+    const bool ok = (uint32_t)page < (uint32_t)c.pages;
+    uint2 p = *reinterpret_cast<const uint2*>(
+        c.par + 4 * c.row(ok ? page : 0, hk, (kb * KB + lane) & pmask));
+    if (!ok) p = make_uint2(0, 0);
+    return p;
+  };
+  // E, F: the scaling of the block before
+  auto prepare = [&](int kb, int page, uint2 p, int E, int F) {
+    typename Stage<D>::Par& P = S.par[kb & 3];
+    const bool ok = (uint32_t)page < (uint32_t)c.pages;
+    const float sk = fp16_bits_to_f32((uint16_t)p.x), zk = (float)(int16_t)(p.x >> 16);
+    const float sv = fp16_bits_to_f32((uint16_t)p.y), zv = (float)(int16_t)(p.y >> 16);
+    // keys: A (8192 + |z|) stays below 2^28: A below 2^15, the pieces of A z 2^-13 as well
+    const float kt = wave_top(sk * (8192.0f + fabsf(zk)));
+    if (__builtin_amdgcn_ldexpf(kt, -E) >= 0x1p28f) E = __builtin_amdgcn_frexp_expf(kt) - 25;
+    const float ka = __builtin_amdgcn_ldexpf(sk, -E);
+    const Pieces u = pieces(ka * zk * 0x1p-13f);
+    P.z[lane] = make_uint4(pk_f16(u.h1, u.h1), pk_f16(u.h2, u.h1), pk_f16(u.h2, u.h3), 0);
+    P.a[lane] = pk_f16(ka, ka * 0.0625f);
+    // values: A (16 + |z|) stays below 2^19
+    const float vt = wave_top(sv * (16.0f + fabsf(zv)));
+    if (vt > 0.0f) F = max(F, __builtin_amdgcn_frexp_expf(vt) - 19);
+    const float va = __builtin_amdgcn_ldexpf(sv, -F);
+    P.ab[lane] = pk_f16(va, -va * zv * 0x1p-9f);
+    const uint64_t vm = __builtin_amdgcn_ballot_w64(ok);
+    if (lane == 0) {
+      P.E = E;
+      P.F = F;
+      P.valid[0] = (uint32_t)vm;
+      P.valid[1] = (uint32_t)(vm >> 32);
+    }
+    return make_int2(E, F);
   };
   const bool any = kb0 < kb1;
+  const int kbl = kb1 - 1;  // (past the last block the last is loaded and staged again: no branches)
+  // each wave's own blocks of parameters: kb0 + 3 + wave and every eighth from there
+  int page0 = -1, page1 = -1;
+  uint2 par0 = make_uint2(0, 0);
+  int fpage[3];      // wave 0: the first three blocks, too
+  uint2 fpar[3];
   if (any) {
-    load_ids();
-    load(kb0);
+    page0 = page_of(kb0 + 3 + wave);
+    page1 = page_of(kb0 + 11 + wave);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) fpage[i] = page_of(kb0 + i);
+    find_pages(kpg, kb0 * KB);
+    vpg = kpg;
+    load_k(kb0);
+    load_v(kb0);
+    par0 = params(kb0 + 3 + wave, page0);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) fpar[i] = params(kb0 + i, fpage[i]);
   }
 
-  // ---- queries: channels D / 2 h .. of the row, rotated, scaled by a power of two into fp16
+  // ---- queries: channels D / 2 h .. of the row, rotated, times sm_scale log2(e) 2^(E + 9)
   uint32_t qb[NS][4], zb[4] = {0, 0, 0, 0};
-  float qscale;
+  int E;
   {
     float x[D / 2];
     const uint4* src = reinterpret_cast<const uint4*>(a.q + (int64_t)(w.s.q0 + tok) * a.ldq +
@@ -936,25 +978,37 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
         x[i] = hadamard_norm<D>() * (h ? p - x[i] : x[i] + p);
       }
     }
+    // E: the largest query at 2^4 at most, unless the first block's keys would leave their range
     float qm = 0.0f;
 #pragma unroll
     for (int i = 0; i < D / 2; ++i) qm = fmaxf(qm, fabsf(x[i]));
-    qm = fmaxf(qm, __shfl_xor(qm, 32));
-    const int e15 = 15 - __builtin_amdgcn_frexp_expf(qm);
-    qscale = __builtin_amdgcn_ldexpf(a.sm_scale * LOG2E, 24 - e15);
+    qm = wave_top(qm);
+    const float sm2 = a.sm_scale * LOG2E;
+    const float kt = wave_top(any ? fp16_bits_to_f32((uint16_t)fpar[0].x) *
+                                        (8192.0f + fabsf((float)(int16_t)(fpar[0].x >> 16)))
+                                  : 0.0f);
+    if (lane == 0) s_qm[wave] = qm;
+    __syncthreads();
+    qm = s_qm[0];
+#pragma unroll
+    for (int k = 1; k < 8; ++k) qm = fmaxf(qm, s_qm[k]);
+    E = uniform(-5 - __builtin_amdgcn_frexp_expf(qm) - __builtin_amdgcn_frexp_expf(sm2));
+    if (kt > 0.0f) E = max(E, uniform(__builtin_amdgcn_frexp_expf(kt)) - 25);
     float sum = 0.0f;
 #pragma unroll
     for (int s = 0; s < NS; ++s)
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const h2_t p = {(_Float16)__builtin_amdgcn_ldexpf(x[8 * s + k], e15),
-                        (_Float16)__builtin_amdgcn_ldexpf(x[8 * s + k + 4], e15)};
+        const float lo = __builtin_amdgcn_ldexpf(sm2 * x[8 * s + k], E + 9);
+        const float hi = __builtin_amdgcn_ldexpf(sm2 * x[8 * s + k + 4], E + 9);
+        const h2_t p = {(_Float16)__builtin_amdgcn_fmed3f(lo, -65504.0f, 65504.0f),
+                        (_Float16)__builtin_amdgcn_fmed3f(hi, -65504.0f, 65504.0f)};
         sum += (float)p.x + (float)p.y;
         qb[s][k] = __builtin_bit_cast(uint32_t, p);
       }
     sum += __shfl_xor(sum, 32);
     if (!h) {
-      const Pieces v = pieces(sum * -0x1p-7f);
+      const Pieces v = pieces(__builtin_amdgcn_fmed3f(-16.0f * sum, -65504.0f, 65504.0f));
       zb[0] = pk_f16(v.h1, v.h2);
       zb[1] = pk_f16(v.h1, v.h3);
       zb[2] = pk_f16(v.h2, v.h1);
@@ -966,99 +1020,174 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
   for (int d = 0; d < ND; ++d)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
-  float m = LOWEST, l = 0.0f;
-  int F = -200;
+  f16_t neg;  // -m in every register: what the score products start from
+#pragma unroll
+  for (int r = 0; r < 16; ++r) neg[r] = 0.0f;
+  float l = 0.0f;
+  int Eq = E, Fo = -200;  // the scaling that the queries and the outputs carry
 
-  if (any) store(st[0]);
-  __syncthreads();
-  for (int kb = kb0; kb < kb1; ++kb) {
-    if (kb + 1 < kb1) load(kb + 1);
-    const Stage<D>& S = st[(kb - kb0) & 1];
-    if (live && kb * KB <= pmax) {
-      const float scl = __builtin_amdgcn_ldexpf(qscale, __builtin_amdgcn_readfirstlane(S.E));
-      const uint32_t valid[2] = {(uint32_t)__builtin_amdgcn_readfirstlane(S.valid[0]),
-                                 (uint32_t)__builtin_amdgcn_readfirstlane(S.valid[1])};
-      const int Fb = __builtin_amdgcn_readfirstlane(S.F);
-      if (Fb != F) {
-        const float f = __builtin_amdgcn_ldexpf(1.0f, max(F - Fb, -150));
+  // QK of a tile of 32 positions in slot `slot`
+  auto scores = [&](int kb, int slot, int tt, f16_t& s) {
+    s = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+        __builtin_bit_cast(h8_t, S.par[kb & 3].z[32 * tt + ql]),
+        __builtin_bit_cast(h8_t, make_uint4(zb[0], zb[1], zb[2], zb[3])), neg, 0, 0, 0);
 #pragma unroll
-        for (int d = 0; d < ND; ++d) o[d] *= f;
-        F = Fb;
+    for (int k = 0; k < NS; ++k) {
+      const uint4 kk = *reinterpret_cast<const uint4*>(S.k[slot] + (32 * tt + ql) * KROW + D * h + 16 * k);
+      s = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+          __builtin_bit_cast(h8_t, kk),
+          __builtin_bit_cast(h8_t, make_uint4(qb[k][0], qb[k][1], qb[k][2], qb[k][3])), s, 0, 0, 0);
+    }
+  };
+  uint32_t wb[2][4];
+  auto weights = [&](const f16_t& s, float sum) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const h2_t p = {(_Float16)__builtin_amdgcn_exp2f(s[8 * k + 2 * j]),
+                        (_Float16)__builtin_amdgcn_exp2f(s[8 * k + 2 * j + 1])};
+        sum = __builtin_amdgcn_fdot2(p, h2_t{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
+        wb[k][j] = __builtin_bit_cast(uint32_t, p);
       }
-      f16_t s[2];
+    return sum;
+  };
+  auto mask = [&](f16_t& s, int k0, uint32_t valid) {
+    if (k0 + 31 > pmin || valid != 0xFFFFFFFFu) {
+      const uint32_t vm = valid >> (4 * h);
+      const int lim = pos - k0 - 4 * h;
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[tt][r] = 0.0f;
-        s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-            __builtin_bit_cast(h8_t, S.z[32 * tt + ql]),
-            __builtin_bit_cast(h8_t, make_uint4(zb[0], zb[1], zb[2], zb[3])), s[tt], 0, 0, 0);
-#pragma unroll
-        for (int k = 0; k < NS; ++k) {
-          const uint4 kk = *reinterpret_cast<const uint4*>(S.k + (32 * tt + ql) * KROW + D * h + 16 * k);
-          s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-              __builtin_bit_cast(h8_t, kk),
-              __builtin_bit_cast(h8_t, make_uint4(qb[k][0], qb[k][1], qb[k][2], qb[k][3])), s[tt], 0, 0, 0);
-        }
-      }
-#pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        // ---- one tile of 32 positions: mask, reference maximum, weights, value product
-        const int k0 = kb * KB + 32 * tt;
-        if (k0 + 31 > pmin || valid[tt] != 0xFFFFFFFFu) {
-          const uint32_t vm = valid[tt] >> (4 * h);
-          const int lim = pos - k0 - 4 * h;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int j = 8 * (r >> 2) + (r & 3);
-            if (j > lim || !((vm >> j) & 1)) s[tt][r] = -__builtin_inff();
-          }
-        }
-        float top = s[tt][0];
-#pragma unroll
-        for (int r = 1; r < 16; ++r) top = fmaxf(top, s[tt][r]);
-        if (__builtin_amdgcn_ballot_w64(__builtin_fmaf(top, scl, -m) > TOP)) {
-          top = fmaxf(top, __shfl_xor(top, 32));
-          const float mn = fmaxf(m, __builtin_fmaf(top, scl, -MID));
-          const float f = __builtin_amdgcn_exp2f(m - mn);
-          m = mn;
-          l *= f;
-#pragma unroll
-          for (int d = 0; d < ND; ++d) o[d] *= f;
-        }
-        uint32_t wb[2][4];
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float x0 = __builtin_fmaf(s[tt][8 * k + 2 * j], scl, -m);
-            const float x1 = __builtin_fmaf(s[tt][8 * k + 2 * j + 1], scl, -m);
-            const h2_t p = {(_Float16)__builtin_amdgcn_exp2f(x0), (_Float16)__builtin_amdgcn_exp2f(x1)};
-            l = __builtin_amdgcn_fdot2(p, h2_t{(_Float16)1.0f, (_Float16)1.0f}, l, false);
-            wb[k][j] = __builtin_bit_cast(uint32_t, p);
-          }
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-          for (int d = 0; d < ND; ++d) {
-            const uint4 vv = *reinterpret_cast<const uint4*>(S.v + (32 * d + ql) * VROW +
-                                                             2 * (16 * (2 * tt + k) + 8 * h));
-            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                __builtin_bit_cast(h8_t, vv),
-                __builtin_bit_cast(h8_t, make_uint4(wb[k][0], wb[k][1], wb[k][2], wb[k][3])), o[d], 0, 0, 0);
-          }
+      for (int r = 0; r < 16; ++r) {
+        const int j = 8 * (r >> 2) + (r & 3);
+        if (j > lim || !((vm >> j) & 1)) s[r] = -__builtin_inff();
       }
     }
-    if (kb + 1 < kb1) store(st[(kb + 1 - kb0) & 1]);
-    __syncthreads();
+  };
+  // After the weights of `s`: rows that met their first position, or a weight beyond the range,
+  // move their reference, also under the scores `t` that were formed meanwhile.
+  auto settle = [&](f16_t& s, f16_t& t, float sum) {
+    if (__builtin_amdgcn_ballot_w64(!(sum > 0.0f && sum < HUGE_SUM))) {
+      float top = s[0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float both = l + __shfl_xor(l, 32);
+      const bool move = top > -__builtin_inff() && (both == 0.0f || top > MID + 8.0f);
+      const float by = move ? top - MID : 0.0f;
+      const float f = both == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(-by);
+      l *= f;
+#pragma unroll
+      for (int d = 0; d < ND; ++d) o[d] *= f;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[r] -= by;
+        t[r] -= by;
+        neg[r] -= by;
+      }
+      sum = weights(s, l);
+    }
+    l = sum;
+  };
+  auto values = [&](int slot, int tt) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int d = 0; d < ND; ++d) {
+        const uint4 vv = *reinterpret_cast<const uint4*>(S.v[slot] + (32 * d + ql) * VROW +
+                                                         2 * (16 * (2 * tt + k) + 8 * h));
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+            __builtin_bit_cast(h8_t, vv),
+            __builtin_bit_cast(h8_t, make_uint4(wb[k][0], wb[k][1], wb[k][2], wb[k][3])), o[d], 0, 0, 0);
+      }
+  };
+  auto rescale_q = [&](int to) {
+    for (; Eq < to; Eq = min(Eq + 15, to)) {
+      const _Float16 f = (_Float16)__builtin_amdgcn_ldexpf(1.0f, min(to - Eq, 15));
+      auto grow = [&](uint32_t& x) {
+        const h2_t p = __builtin_bit_cast(h2_t, x) * h2_t{f, f};
+        const h2_t top = {(_Float16)65504.0f, (_Float16)65504.0f};
+        x = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_elementwise_min(p, top), -top));
+      };
+#pragma unroll
+      for (int k = 0; k < NS; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) grow(qb[k][j]);
+#pragma unroll
+      for (int j = 0; j < 3; ++j) grow(zb[j]);
+    }
+  };
+
+  // Pipeline: while a tile's weights are formed, the next tile's scores are on the matrix cores;
+  // while its values are, the codes of later blocks go to LDS: keys two blocks ahead (their first
+  // tile's scores run in the block before), values one; parameters three ahead.
+  if (any) {
+    if (wave == 0) {
+      int2 ef = make_int2(E, -200);
+#pragma unroll
+      for (int i = 0; i < 3; ++i) ef = prepare(kb0 + i, fpage[i], fpar[i], ef.x, ef.y);
+    }
+    lds_barrier();
+    store_k(kb0, 0);
+    load_k(min(kb0 + 1, kbl));
+    store_v(kb0, 0);
+    store_k(kb0 + 1, 1);
+    // (keys, then values, as in the loop: the waits count the loads issued later)
+    load_k(min(kb0 + 2, kbl));
+    load_v(min(kb0 + 1, kbl));
+    auto meta = [&](int kb) {  // E, F, valid
+      const int4 x = *reinterpret_cast<const int4*>(&S.par[kb & 3].E);
+      return make_int4(uniform(x.x), uniform(x.y), uniform(x.z), uniform(x.w));
+    };
+    int4 now = meta(kb0);
+    rescale_q(now.x);
+    lds_barrier();
+    f16_t s0, s1;
+    scores(kb0, 0, 0, s0);
+    int sl = 0, vs = 0;  // slots of this block's keys and values
+    for (int kb = kb0; kb < kb1; ++kb) {
+      const int sl1 = sl == 2 ? 0 : sl + 1, sl2 = sl1 == 2 ? 0 : sl1 + 1;
+      const int4 next = meta(kb + 1);
+      if (now.y != Fo) {
+        const float f = __builtin_amdgcn_ldexpf(1.0f, max(Fo - now.y, -150));
+#pragma unroll
+        for (int d = 0; d < ND; ++d) o[d] *= f;
+        Fo = now.y;
+      }
+      mask(s0, kb * KB, (uint32_t)now.z);
+      scores(kb, sl, 1, s1);
+      float sum = weights(s0, l);
+      settle(s0, s1, sum);
+      values(vs, 0);
+      store_k(kb + 2, sl2);
+      load_k(min(kb + 3, kbl));
+      mask(s1, kb * KB + 32, (uint32_t)now.w);
+      rescale_q(next.x);
+      scores(kb + 1, sl1, 0, s0);
+      sum = weights(s1, l);
+      settle(s1, s0, sum);
+      values(vs, 1);
+      store_v(kb + 1, vs ^ 1);
+      load_v(min(kb + 2, kbl));
+      if (((kb - kb0) & 7) == wave) {
+        const int4 before = meta(kb + 2);
+        prepare(kb + 3, page0, par0, before.x, before.y);
+        page0 = page1;
+        par0 = params(kb + 11, page0);
+        page1 = page_of(kb + 19);
+      }
+      lds_barrier();
+      now = next;
+      sl = sl1;
+      vs ^= 1;
+    }
   }
-  if (!live) return;
+  if (wrow > last) return;
   l += __shfl_xor(l, 32);
 
   // ---- channels: o[d][r] is channel 8 word + nibble of V^T's row 32 d + 8 (r / 4) + 4 h + r % 4
   // = nibble * D / 8 + word
   const bool mine = wrow + ql <= last;
-  const float back = __builtin_amdgcn_ldexpf(1.0f, F + 9);  // (0 where nothing was met)
+  const float back = __builtin_amdgcn_ldexpf(1.0f, Fo + 9);  // (0 where nothing was met)
   auto word = [&](int j, float* y) {  // this lane's j-th code word, j < D / 16
 #pragma unroll
     for (int n = 0; n < 8; ++n)
@@ -1068,7 +1197,7 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
     if (!mine) return;
     float* dst = rec + (int64_t)((w.index * c.Hkv + hk) * splits + split) * ROWS * (D + 2);
     const int i = 32 * wave + ql;
-    if (!h) *reinterpret_cast<float2*>(dst + 2 * i) = make_float2(m, l);
+    if (!h) *reinterpret_cast<float2*>(dst + 2 * i) = make_float2(l > 0.0f ? -neg[0] : LOWEST, l);
     dst += 2 * ROWS + i * D;
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) {
