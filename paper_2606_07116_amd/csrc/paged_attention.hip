@@ -887,20 +887,18 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
   };
   // Parameters, lane = position: the page first, then (a turn later) the row's, then its place.
   auto page_of = [&](int kb) {
-    const int key = kb * KB + lane;
-    return key < keys ? table[key >> c.log2p] : -1;
+    return table[min(kb * KB + lane, keys - 1) >> c.log2p];
   };
   auto params = [&](int kb, int page) {
     const bool ok = (uint32_t)page < (uint32_t)c.pages;
-    uint2 p = *reinterpret_cast<const uint2*>(
+    return *reinterpret_cast<const uint2*>(
         c.par + 4 * c.row(ok ? page : 0, hk, (kb * KB + lane) & pmask));
-    if (!ok) p = make_uint2(0, 0);
-    return p;
   };
   // E, F: the scaling of the block before
   auto prepare = [&](int kb, int page, uint2 p, int E, int F) {
     typename Stage<D>::Par& P = S.par[kb & 3];
-    const bool ok = (uint32_t)page < (uint32_t)c.pages;
+    const bool ok = ((uint32_t)page < (uint32_t)c.pages) & (kb * KB + lane < keys);
+    if (!ok) p = make_uint2(0, 0);
     const float sk = fp16_bits_to_f32((uint16_t)p.x), zk = (float)(int16_t)(p.x >> 16);
     const float sv = fp16_bits_to_f32((uint16_t)p.y), zv = (float)(int16_t)(p.y >> 16);
     // keys: A (8192 + |z|) stays below 2^28: A below 2^15, the pieces of A z 2^-13 as well
@@ -929,8 +927,8 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
   // each wave's own blocks of parameters: kb0 + 3 + wave and every eighth from there
   int page0 = -1, page1 = -1;
   uint2 par0 = make_uint2(0, 0);
-  int fpage[3];      // wave 0: the first three blocks, too
-  uint2 fpar[3];
+  int fpage[3] = {-1, -1, -1};  // wave 0: the first three blocks, too
+  uint2 fpar[3] = {};
   if (any) {
     page0 = page_of(kb0 + 3 + wave);
     page1 = page_of(kb0 + 11 + wave);
@@ -984,7 +982,9 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
     for (int i = 0; i < D / 2; ++i) qm = fmaxf(qm, fabsf(x[i]));
     qm = wave_top(qm);
     const float sm2 = a.sm_scale * LOG2E;
-    const float kt = wave_top(any ? fp16_bits_to_f32((uint16_t)fpar[0].x) *
+    const float kt = wave_top(any && (uint32_t)fpage[0] < (uint32_t)c.pages &&
+                                          kb0 * KB + lane < keys
+                                      ? fp16_bits_to_f32((uint16_t)fpar[0].x) *
                                         (8192.0f + fabsf((float)(int16_t)(fpar[0].x >> 16)))
                                   : 0.0f);
     if (lane == 0) s_qm[wave] = qm;
