@@ -32,6 +32,32 @@ struct PagedCache {
   }
 };
 
+// The value of lane ^ X within a row of 16 lanes, without LDS: DPP has the exchanges by 1, 2, 8
+// and 7 (a mirrored half row); by 4 is by 7, then by 3.
+template <int X>
+__device__ __forceinline__ int lane_xor(int v) {
+  static_assert(X == 1 || X == 2 || X == 4 || X == 8, "lane exchange");
+  if constexpr (X == 1) return __builtin_amdgcn_mov_dpp(v, 0xB1, 0xf, 0xf, true);
+  if constexpr (X == 2) return __builtin_amdgcn_mov_dpp(v, 0x4E, 0xf, 0xf, true);
+  if constexpr (X == 4)
+    return __builtin_amdgcn_mov_dpp(__builtin_amdgcn_mov_dpp(v, 0x141, 0xf, 0xf, true), 0x1B, 0xf, 0xf, true);
+  return __builtin_amdgcn_mov_dpp(v, 0x128, 0xf, 0xf, true);
+}
+template <int X>
+__device__ __forceinline__ float lane_xor(float v) {
+  return __builtin_bit_cast(float, lane_xor<X>(__builtin_bit_cast(int, v)));
+}
+
+// op over the LPH (8 or 16) lanes of a row's group, the same in each.
+template <int LPH, class Op>
+__device__ __forceinline__ float group_reduce(float v, Op op) {
+  v = op(v, lane_xor<1>(v));
+  v = op(v, lane_xor<2>(v));
+  v = op(v, lane_xor<4>(v));
+  if constexpr (LPH == 16) v = op(v, lane_xor<8>(v));
+  return v;
+}
+
 // y = H x over the D = 8 * LPH channels that LPH adjacent lanes hold, eight a lane (H the
 // Sylvester Hadamard matrix, unnormalised): channel bits 0..2 inside the lane, the others
 // across the lanes.
@@ -46,14 +72,17 @@ __device__ __forceinline__ void fwht_lanes(float* x, int lane) {
         x[i] = a + b;
         x[i + st] = a - b;
       }
+  const float s1 = lane & 1 ? -1.0f : 1.0f, s2 = lane & 2 ? -1.0f : 1.0f;
+  const float s4 = lane & 4 ? -1.0f : 1.0f, s8 = lane & 8 ? -1.0f : 1.0f;
 #pragma unroll
-  for (int st = 1; st < LPH; st <<= 1) {
-    const bool up = lane & st;
+  for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf(s1, x[i], lane_xor<1>(x[i]));
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float o = __shfl_xor(x[i], st);
-      x[i] = up ? o - x[i] : x[i] + o;
-    }
+  for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf(s2, x[i], lane_xor<2>(x[i]));
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf(s4, x[i], lane_xor<4>(x[i]));
+  if constexpr (LPH == 16) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf(s8, x[i], lane_xor<8>(x[i]));
   }
 }
 

@@ -10,6 +10,8 @@
 // The angle is taken in 64 bits and reduced there: at position 10^6 a 32-bit product is off by
 // 0.03 of a radian.  The key is not rounded to bf16 on the way to its codes.
 // Read: s (c - z), then c H of it where asked, rounded to bf16 once.
+#include <type_traits>
+
 #include "internal.h"
 #include "paged.h"
 
@@ -49,11 +51,8 @@ __device__ __forceinline__ uint32_t quantize_row(const float* x, uint32_t& par) 
     mx = fmaxf(mx, x[i]);
     mn = fminf(mn, x[i]);
   }
-#pragma unroll
-  for (int o = 1; o < LPH; o <<= 1) {
-    mx = fmaxf(mx, __shfl_xor(mx, o));
-    mn = fminf(mn, __shfl_xor(mn, o));
-  }
+  mx = group_reduce<LPH>(mx, [](float a, float b) { return fmaxf(a, b); });
+  mn = group_reduce<LPH>(mn, [](float a, float b) { return fminf(a, b); });
   const QParams p = quant_params(mx, mn);
   const uint32_t lo = __float_as_uint(p.lo);
   uint32_t code = 0;
@@ -63,94 +62,177 @@ __device__ __forceinline__ uint32_t quantize_row(const float* x, uint32_t& par) 
   return code;
 }
 
-// One workgroup per token; a group of D / 8 lanes takes one query head, or the key and the
-// value of one key/value head, at a time.
-template <int D>
-__global__ __launch_bounds__(256) void rope_kv_paged_kernel(RopeKvPagedArgs a, PagedCache c) {
-  constexpr int LPH = D / 8, NG = 256 / LPH;
-  __shared__ float2 s_cs[D / 2];
+// A wave takes one token, or one of `parts` of its heads where tokens are few: 64 / (D / 8) units
+// at a time, a unit being a query head or the key and value of a key/value head, a group of D / 8
+// lanes each.  The token's angles are formed by the wave, one pair a lane, and handed round in
+// LDS; the next units' channels are on their way while one is worked on.
+// FULL: the half layout over the whole head, whose partner channels sit half a group away.
+template <int D, bool FULL>
+__global__ __launch_bounds__(256) void rope_kv_paged_kernel(RopeKvPagedArgs a, PagedCache c, int parts) {
+  constexpr int LPH = D / 8, NG = 64 / LPH;
+  __shared__ alignas(16) float2 s_cs[4][D / 2];
   const int tid = (int)__builtin_amdgcn_workitem_id_x();
-  const int64_t m = __builtin_amdgcn_workgroup_id_x();
-  const int l = tid & (LPH - 1), first = (tid & 63) & ~(LPH - 1);
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t item = (int64_t)__builtin_amdgcn_workgroup_id_x() * 4 + wave;
+  const int64_t m = __builtin_amdgcn_readfirstlane((int)(item / parts));
+  const int part = (int)(item - m * parts);
+  if (m >= a.M) return;
+  const int l = lane & (LPH - 1), g = lane / LPH;
+  const int units = a.Hq + c.Hkv;
+  const uint16_t* row = a.qkv + m * a.ldq + 8 * l;
+  uint4 next, vnext = make_uint4(0, 0, 0, 0);
+  auto fetch = [&](int j) {  // channels of unit j: a query's, or a key's and its value's
+    next = *reinterpret_cast<const uint4*>(row + (int64_t)min(j, units - 1) * D);
+    if (j >= a.Hq)
+      vnext = *reinterpret_cast<const uint4*>(row + (int64_t)min(j + c.Hkv, units + c.Hkv - 1) * D);
+  };
+  int j = part * NG + g;
+  const int step = parts * NG;
+  fetch(j);
   const int half = a.rotary / 2;
-  if (tid < half) s_cs[tid] = turn(a.positions[m], a.inv_freq[tid], a.amplitude);
-  __syncthreads();
+  if (lane < half) s_cs[wave][lane] = turn(a.positions[m], a.inv_freq[lane], a.amplitude);
+  const int64_t slot = a.slots[m];
+  float qw[8], kw[8];
+  if (a.q_weight) load8(a.q_weight + 8 * l, qw);
+  if (a.k_weight) load8(a.k_weight + 8 * l, kw);
+  __builtin_amdgcn_wave_barrier();
   // this lane's part of the rotation: its partner lane (half layout) and its eight angles
   const int shift = half / 8;
-  const bool turns = a.pairs ? 8 * l < a.rotary : l < 2 * shift;
-  const bool upper = !a.pairs && l >= shift;
-  const int partner = first + (turns && !a.pairs ? (upper ? l - shift : l + shift) : l);
+  const bool turns = FULL || (a.pairs ? 8 * l < a.rotary : l < 2 * shift);
+  const bool upper = FULL ? l >= LPH / 2 : !a.pairs && l >= shift;
+  const int partner = (lane & ~(LPH - 1)) + (turns && !a.pairs ? (upper ? l - shift : l + shift) : l);
   float cs[8], sn[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const int k = a.pairs ? 4 * l + i / 2 : 8 * (upper ? l - shift : l) + i;
-    const float2 v = turns ? s_cs[k] : make_float2(1.0f, 0.0f);
+    const int k = FULL ? 8 * (l & (LPH / 2 - 1)) + i : a.pairs ? 4 * l + i / 2 : 8 * (upper ? l - shift : l) + i;
+    const float2 v = turns ? s_cs[wave][k] : make_float2(1.0f, 0.0f);
     cs[i] = v.x;
-    sn[i] = v.y;
+    sn[i] = upper ? v.y : -v.y;  // half layout: x cos + partner * this
   }
-  auto prepared = [&](float* x, const uint16_t* w) {
-    if (w) {
-      float ss = 0.0f, wf[8];
+  auto prepared = [&](float* x, bool normed, const float* w) {
+    if (normed) {
+      float ss = 0.0f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) ss = __builtin_fmaf(x[i], x[i], ss);
-#pragma unroll
-      for (int o = 1; o < LPH; o <<= 1) ss += __shfl_xor(ss, o);
+      ss = group_reduce<LPH>(ss, [](float p, float q) { return p + q; });
       const float inv = 1.0f / __builtin_sqrtf(ss * (1.0f / D) + a.eps);
-      load8(w + 8 * l, wf);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] *= inv * wf[i];
+      for (int i = 0; i < 8; ++i) x[i] *= inv * w[i];
     }
-    if (a.pairs) {
+    if (!FULL && a.pairs) {
 #pragma unroll
       for (int i = 0; i < 8; i += 2) {
         const float p = x[i], q = x[i + 1];
-        x[i] = p * cs[i] - q * sn[i];
-        x[i + 1] = q * cs[i] + p * sn[i];
+        x[i] = p * cs[i] + q * sn[i];
+        x[i + 1] = q * cs[i] - p * sn[i];
       }
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float p = __shfl(x[i], partner);
-        x[i] = upper ? x[i] * cs[i] + p * sn[i] : x[i] * cs[i] - p * sn[i];
+        const float p = FULL ? lane_xor<LPH / 2>(x[i]) : __shfl(x[i], partner);
+        x[i] = __builtin_fmaf(p, sn[i], x[i] * cs[i]);
       }
     }
   };
-  const uint16_t* row = a.qkv + m * a.ldq + 8 * l;
-  const int64_t slot = a.slots[m];
-  for (int j = tid / LPH; j < a.Hq + c.Hkv; j += NG) {
-    float x[8];
-    load8(row + (int64_t)j * D, x);
+  auto unpack = [](const uint4& v, float* x) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      x[2 * k] = bf16_lo(w[k]);
+      x[2 * k + 1] = bf16_hi(w[k]);
+    }
+  };
+  auto rotate = [&](float* x) {
+    fwht_lanes<LPH>(x, l);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] *= hadamard_norm<D>();
+  };
+  for (; j - g < units; j += step) {  // (as long as one of the wave's units is one)
+    float x[8], v[8];
+    unpack(next, x);
+    unpack(vnext, v);
+    fetch(j + step);
     if (j < a.Hq) {
-      prepared(x, a.q_weight);
+      prepared(x, a.q_weight, qw);
       store8(a.q_out + m * a.ldo + (int64_t)j * D + 8 * l, x);
-      continue;
+    } else if (j < units) {
+      uint32_t kp, vp;
+      prepared(x, a.k_weight, kw);
+      if (a.k_had) rotate(x);
+      const uint32_t kc = quantize_row<LPH>(x, kp);
+      if (a.v_had) rotate(v);
+      const uint32_t vc = quantize_row<LPH>(v, vp);
+      if (c.holds(slot)) {
+        const int64_t r = c.slot_row(slot, j - a.Hq);
+        reinterpret_cast<uint32_t*>(c.kc + r * (D / 2))[l] = kc;
+        reinterpret_cast<uint32_t*>(c.vc + r * (D / 2))[l] = vc;
+        if (l == 0) *reinterpret_cast<uint2*>(c.par + 4 * r) = make_uint2(kp, vp);
+      }
     }
-    const int h = j - a.Hq;
-    uint32_t kp, vp;
-    prepared(x, a.k_weight);
-    if (a.k_had) {
-      fwht_lanes<LPH>(x, l);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] *= hadamard_norm<D>();
-    }
-    const uint32_t kw = quantize_row<LPH>(x, kp);
-    load8(row + (int64_t)(j + c.Hkv) * D, x);
-    if (a.v_had) {
-      fwht_lanes<LPH>(x, l);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] *= hadamard_norm<D>();
-    }
-    const uint32_t vw = quantize_row<LPH>(x, vp);
-    if (!c.holds(slot)) continue;
-    const int64_t r = c.slot_row(slot, h);
-    reinterpret_cast<uint32_t*>(c.kc + r * (D / 2))[l] = kw;
-    reinterpret_cast<uint32_t*>(c.vc + r * (D / 2))[l] = vw;
-    if (l == 0) *reinterpret_cast<uint2*>(c.par + 4 * r) = make_uint2(kp, vp);
   }
 }
 
-// A group of D / 8 lanes per (row, head).
-template <int D>
+typedef _Float16 h2_t __attribute__((ext_vector_type(2)));
+
+// A group of D / 8 lanes per row, a code word (8 channels) each, so that a store writes the row's
+// 2 D bytes in one piece (with four lanes of 32 channels, which need half the exchanges, 64-byte
+// pieces: 137 us against 132 without a rotation, 131072 rows of 8 heads).  A masked word holds two
+// codes as fp16 subnormals c 2^-24, in which sums of up to 128 codes are exact: the rotation runs
+// on them as packed halves; the zero-point, whose rotation is D z in channel 0 and nothing
+// elsewhere, comes after it; and one multiplication by s turns a half into a value.
+template <int D, bool HAD, bool NT>
+__device__ __forceinline__ void dequantize_row(uint32_t w, uint32_t par, int l, uint16_t* out) {
+  constexpr int LPH = D / 8;
+  const float s = fp16_bits_to_f32((uint16_t)par), z = (float)(int16_t)(par >> 16);
+  h2_t h[4];  // channels 8 l + i and + i + 4
+#pragma unroll
+  for (int i = 0; i < 4; ++i) h[i] = __builtin_bit_cast(h2_t, (w >> (4 * i)) & 0x000F000Fu);
+  if constexpr (HAD) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = h2_t{h[i].x, h[i].x} + h2_t{h[i].y, -h[i].y};  // channel bit 2
+#pragma unroll
+    for (int st = 1; st < 4; st <<= 1)  // bits 0, 1
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (!(i & st)) {
+          const h2_t p = h[i], q = h[i + st];
+          h[i] = p + q;
+          h[i + st] = p - q;
+        }
+    auto across = [&](auto x) {  // a channel bit above them
+      constexpr int X = decltype(x)::value;
+      const _Float16 sign = l & X ? -1.0f : 1.0f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        h[i] = __builtin_elementwise_fma(
+            h2_t{sign, sign}, h[i], __builtin_bit_cast(h2_t, lane_xor<X>(__builtin_bit_cast(int, h[i]))));
+    };
+    across(std::integral_constant<int, 1>{});
+    across(std::integral_constant<int, 2>{});
+    across(std::integral_constant<int, 4>{});
+    if constexpr (LPH == 16) across(std::integral_constant<int, 8>{});
+  }
+  const float k = s * (HAD ? hadamard_norm<D>() : 1.0f);
+  const float kk = k * 0x1p24f, sub = HAD ? 0.0f : -s * z;
+  float y[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    y[i] = __builtin_fmaf((float)h[i].x, kk, sub);
+    y[i + 4] = __builtin_fmaf((float)h[i].y, kk, sub);
+  }
+  if (HAD && l == 0) y[0] = __builtin_fmaf((float)h[0].x, 0x1p24f, -z * D) * k;
+  if constexpr (NT) {
+    typedef uint32_t u4_t __attribute__((ext_vector_type(4)));
+    const u4_t v = {bf16x2_rne(y[0], y[1]), bf16x2_rne(y[2], y[3]), bf16x2_rne(y[4], y[5]),
+                    bf16x2_rne(y[6], y[7])};
+    __builtin_nontemporal_store(v, reinterpret_cast<u4_t*>(out));
+  } else {
+    store8(out, y);
+  }
+}
+
+// NT: non-temporal stores.
+template <int D, bool NT>
 __global__ __launch_bounds__(256) void kv_dequantize_paged_kernel(
     PagedCache c, const int64_t* __restrict__ slots, int64_t M, int k_had, int v_had,
     uint16_t* __restrict__ k_out, int64_t ldk, uint16_t* __restrict__ v_out, int64_t ldv) {
@@ -165,32 +247,40 @@ __global__ __launch_bounds__(256) void kv_dequantize_paged_kernel(
   if (!c.holds(slot)) return;
   const int64_t r = c.slot_row(slot, h);
   const uint2 par = *reinterpret_cast<const uint2*>(c.par + 4 * r);
-  auto one = [&](const uint8_t* codes, uint32_t p, int had, uint16_t* out, int64_t ld) {
-    const uint32_t w = reinterpret_cast<const uint32_t*>(codes + r * (D / 2))[l];
-    const float s = fp16_bits_to_f32((uint16_t)p);
-    const int z = (int16_t)(p >> 16);
-    float x[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = s * (float)((int)((w >> (4 * i)) & 15u) - z);
-    if (had) {
-      fwht_lanes<LPH>(x, l);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] *= hadamard_norm<D>();
-    }
-    store8(out + m * ld + (int64_t)h * D + 8 * l, x);
-  };
-  if (k_out) one(c.kc, par.x, k_had, k_out, ldk);
-  if (v_out) one(c.vc, par.y, v_had, v_out, ldv);
+  const uint32_t kw = reinterpret_cast<const uint32_t*>(c.kc + r * (D / 2))[l];
+  const uint32_t vw = reinterpret_cast<const uint32_t*>(c.vc + r * (D / 2))[l];
+  const int64_t at = (int64_t)h * D + 8 * l;
+  if (k_out) {
+    if (k_had) dequantize_row<D, true, NT>(kw, par.x, l, k_out + m * ldk + at);
+    else dequantize_row<D, false, NT>(kw, par.x, l, k_out + m * ldk + at);
+  }
+  if (v_out) {
+    if (v_had) dequantize_row<D, true, NT>(vw, par.y, l, v_out + m * ldv + at);
+    else dequantize_row<D, false, NT>(vw, par.y, l, v_out + m * ldv + at);
+  }
 }
 
 }  // namespace
 
 hipError_t launch_rope_kv_paged(const RopeKvPagedArgs& a, const PagedCache& c, int head_dim,
                                 hipStream_t stream) {
-  if (head_dim == 128)
-    hipLaunchKernelGGL(rope_kv_paged_kernel<128>, dim3((unsigned)a.M), dim3(256), 0, stream, a, c);
-  else
-    hipLaunchKernelGGL(rope_kv_paged_kernel<64>, dim3((unsigned)a.M), dim3(256), 0, stream, a, c);
+  const int ng = 64 / (head_dim / 8);
+  const int64_t rounds = (a.Hq + c.Hkv + ng - 1) / ng;
+  // a token's heads go to several waves until there are 4096 of them, 16 a CU
+  int64_t parts = (4096 + a.M - 1) / a.M;
+  parts = parts < 1 ? 1 : parts > rounds ? rounds : parts;
+  const dim3 grid((unsigned)((a.M * parts + 3) / 4));
+  const bool full = !a.pairs && a.rotary == head_dim;
+#define OFFQ_ROPE(D_, F_) \
+  hipLaunchKernelGGL((rope_kv_paged_kernel<D_, F_>), grid, dim3(256), 0, stream, a, c, (int)parts)
+  if (head_dim == 128) {
+    if (full) OFFQ_ROPE(128, true);
+    else OFFQ_ROPE(128, false);
+  } else {
+    if (full) OFFQ_ROPE(64, true);
+    else OFFQ_ROPE(64, false);
+  }
+#undef OFFQ_ROPE
   return hipGetLastError();
 }
 
@@ -200,9 +290,13 @@ hipError_t launch_kv_dequantize_paged(const PagedCache& c, int head_dim, const i
                                       hipStream_t stream) {
   const int ng = 256 / (head_dim / 8);
   const unsigned grid = (unsigned)((M * c.Hkv + ng - 1) / ng);
-  hipLaunchKernelGGL(head_dim == 128 ? kv_dequantize_paged_kernel<128> : kv_dequantize_paged_kernel<64>,
-                     dim3(grid), dim3(256), 0, stream, c, slots, M, k_had ? 1 : 0, v_had ? 1 : 0,
-                     k_out, ldk, v_out, ldv);
+  // Outputs beyond the L2s' 32 MB bypass them (131072 rows of 8 heads: 164 -> 154 us); smaller ones
+  // stay for the next kernel (5000 rows: 8 us either way).
+  const bool nt = 2 * M * c.Hkv * head_dim * ((k_out != nullptr) + (v_out != nullptr)) > (32 << 20);
+  auto kernel = head_dim == 128 ? nt ? kv_dequantize_paged_kernel<128, true> : kv_dequantize_paged_kernel<128, false>
+                                : nt ? kv_dequantize_paged_kernel<64, true> : kv_dequantize_paged_kernel<64, false>;
+  hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, stream, c, slots, M, k_had ? 1 : 0,
+                     v_had ? 1 : 0, k_out, ldk, v_out, ldv);
   return hipGetLastError();
 }
 
