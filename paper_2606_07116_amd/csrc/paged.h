@@ -48,6 +48,58 @@ __device__ __forceinline__ float lane_xor(float v) {
   return __builtin_bit_cast(float, lane_xor<X>(__builtin_bit_cast(int, v)));
 }
 
+// One Hadamard butterfly across the lanes l and l ^ X of a wave: sums below, differences above.
+template <int X>
+__device__ __forceinline__ float lane_butterfly(float v, int lane) {
+  const float sign = lane & X ? -1.0f : 1.0f;
+  if constexpr (X < 16) {
+    return __builtin_fmaf(sign, v, lane_xor<X>(v));
+  } else {  // (the exchange of rows gives both lanes' values in both lanes)
+    const uint32_t u = __float_as_uint(v);
+    const auto r = X == 16 ? __builtin_amdgcn_permlane16_swap(u, u, false, false)
+                           : __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return __builtin_fmaf(sign, __uint_as_float(r[1]), __uint_as_float(r[0]));
+  }
+}
+
+// Over a wave, the same in every lane.
+__device__ __forceinline__ float wave_sum(float v) {
+  v += lane_xor<1>(v);
+  v += lane_xor<2>(v);
+  v += lane_xor<4>(v);
+  v += lane_xor<8>(v);
+  const int i = __builtin_bit_cast(int, v);
+  auto row = [&](int l) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(i, l)); };
+  return (row(0) + row(16)) + (row(32) + row(48));
+}
+__device__ __forceinline__ float wave_max(float v) {
+  v = fmaxf(v, lane_xor<1>(v));
+  v = fmaxf(v, lane_xor<2>(v));
+  v = fmaxf(v, lane_xor<4>(v));
+  v = fmaxf(v, lane_xor<8>(v));
+  const int i = __builtin_bit_cast(int, v);
+  auto row = [&](int l) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(i, l)); };
+  return fmaxf(fmaxf(row(0), row(16)), fmaxf(row(32), row(48)));
+}
+__device__ __forceinline__ int wave_add(int v) {
+  v += lane_xor<1>(v);
+  v += lane_xor<2>(v);
+  v += lane_xor<4>(v);
+  v += lane_xor<8>(v);
+  return (__builtin_amdgcn_readlane(v, 0) + __builtin_amdgcn_readlane(v, 16)) +
+         (__builtin_amdgcn_readlane(v, 32) + __builtin_amdgcn_readlane(v, 48));
+}
+// The sum over the lanes up to this one.
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // within rows of 16 lanes
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // rows 0 and 2 into 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // the first half into the second
+  return v;
+}
+
 // op over the LPH (8 or 16) lanes of a row's group, the same in each.
 template <int LPH, class Op>
 __device__ __forceinline__ float group_reduce(float v, Op op) {

@@ -23,17 +23,6 @@ typedef float f4_t __attribute__((ext_vector_type(4)));
 constexpr float TAU = 8.0f;     // a row's reference maximum may lag by up to 2^TAU
 constexpr float LOWEST = -1e30f;  // a reference maximum below every score
 
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
-  return v;
-}
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o);
-  return v;
-}
-
 // (a uniform value that went through the vector units, a division for instance)
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
@@ -81,16 +70,6 @@ struct Chunking {
   Seq s;
 };
 
-// Sum and maximum over a wave, the same in every lane.
-__device__ __forceinline__ int wave_add(int v) {
-  v += __builtin_amdgcn_mov_dpp(v, 0x128, 0xf, 0xf, true);  // rotations within rows of 16 lanes
-  v += __builtin_amdgcn_mov_dpp(v, 0x124, 0xf, 0xf, true);
-  v += __builtin_amdgcn_mov_dpp(v, 0x122, 0xf, 0xf, true);
-  v += __builtin_amdgcn_mov_dpp(v, 0x121, 0xf, 0xf, true);
-  return (__builtin_amdgcn_readlane(v, 0) + __builtin_amdgcn_readlane(v, 16)) +
-         (__builtin_amdgcn_readlane(v, 32) + __builtin_amdgcn_readlane(v, 48));
-}
-
 // The chunk length, and what unit `unit` is.  `slots` workgroups are resident at once.  One round
 // of units costs its longest chunk, so the shortest length whose units fit the slots is tried
 // first; where it is far above the mean (a few long sequences among many), chunks of half the
@@ -136,12 +115,7 @@ __device__ __forceinline__ Chunking find_chunk(const PagedAttentionArgs& a, int 
   for (int b0 = 0; b0 < a.B; b0 += 64) {
     if (a.B > 64) load(b0 + lane);
     const int nc = chunks(c.len);
-    int incl = nc;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int p = __shfl_up(incl, o);
-      if (lane >= o) incl += p;
-    }
+    const int incl = wave_scan(nc);
     const int first = base + incl - nc;
     const uint64_t mine = __builtin_amdgcn_ballot_w64(nc > 0 && unit >= Hkv * first && unit < Hkv * (first + nc));
     if (mine) {
@@ -185,13 +159,13 @@ __device__ __forceinline__ void rotate_wave(float (&x)[D / 64], int lane) {
     x[1] = q;
   }
 #pragma unroll
-  for (int st = 1; st < 64; st <<= 1) {
-    const bool up = lane & st;
-#pragma unroll
-    for (int e = 0; e < D / 64; ++e) {
-      const float o = __shfl_xor(x[e], st);
-      x[e] = up ? o - x[e] : x[e] + o;
-    }
+  for (int e = 0; e < D / 64; ++e) {
+    x[e] = lane_butterfly<1>(x[e], lane);
+    x[e] = lane_butterfly<2>(x[e], lane);
+    x[e] = lane_butterfly<4>(x[e], lane);
+    x[e] = lane_butterfly<8>(x[e], lane);
+    x[e] = lane_butterfly<16>(x[e], lane);
+    x[e] = lane_butterfly<32>(x[e], lane);
   }
 #pragma unroll
   for (int e = 0; e < D / 64; ++e) x[e] *= hadamard_norm<D>();
@@ -223,8 +197,8 @@ kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, 
   } u;
   // per wave and position: (score slope, score offset / sum q), (sv, zv)
   __shared__ alignas(16) float2 s_kp[4][32], s_vp[4][32];
-  __shared__ float s_qsum[16 * RT], s_qmax[4];
-  __shared__ float s_m[4][16 * RT], s_l[4][16 * RT], s_z[4][16 * RT], s_scale[4];
+  __shared__ float s_qsum[16 * RT], s_slope[16 * RT];
+  __shared__ float s_m[4][16 * RT], s_l[4][16 * RT], s_z[4][16 * RT];
 
   const int tid = (int)__builtin_amdgcn_workitem_id_x();
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -289,57 +263,52 @@ kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, 
   const bool any = k_begin < k_stop;
   if (any) load_block(k_begin, blk[0]);
 
-  // ---- queries: rotated, scaled by one power of two into the fp16 range, in operand order
+  // ---- queries: rotated, scaled by a power of two into the fp16 range, in operand order.  (A
+  // loop that stays one: unrolled, the code of the sixteen or more rows costs more to fetch than
+  // its work.)
   {
-    constexpr int PER = 4 * RT;  // rows of a wave
-    float x[PER][D / 64];
-    float qm = 0.0f;
+    uint32_t next = 0;
+    auto fetch = [&](int r) {
+      const uint16_t* src = a.q + (int64_t)(w.s.q0 + r / G) * a.ldq + (int64_t)(hk * G + r % G) * D;
+      if constexpr (D == 128) next = reinterpret_cast<const uint32_t*>(src)[lane];
+      else next = src[lane];
+    };
+    if (wave < rows) fetch(wave);
+#pragma unroll 1
+    for (int r = wave; r < rows; r += 4) {
+      float x[D / 64], qm = 0.0f, sum = 0.0f;
+      x[0] = bf16_lo(next);
+      if constexpr (D == 128) x[1] = bf16_hi(next);
+      if (r + 4 < rows) fetch(r + 4);
+      if (a.k_had) rotate_wave<D>(x, lane);
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int r = wave + 4 * i;
-#pragma unroll
-      for (int e = 0; e < D / 64; ++e) x[i][e] = 0.0f;
-      if (r < rows) {
-        const uint16_t* src = a.q + (int64_t)(w.s.q0 + r / G) * a.ldq + (int64_t)(hk * G + r % G) * D;
-        if constexpr (D == 128) {
-          const uint32_t t = reinterpret_cast<const uint32_t*>(src)[lane];
-          x[i][0] = bf16_lo(t);
-          x[i][1] = bf16_hi(t);
-        } else {
-          x[i][0] = bf16_lo(src[lane]);
-        }
-        if (a.k_had) rotate_wave<D>(x[i], lane);
-      }
-#pragma unroll
-      for (int e = 0; e < D / 64; ++e) qm = fmaxf(qm, fabsf(x[i][e]));
-    }
-    qm = wave_max(qm);
-    if (lane == 0) s_qmax[wave] = qm;
-    __syncthreads();
-    qm = fmaxf(fmaxf(s_qmax[0], s_qmax[1]), fmaxf(s_qmax[2], s_qmax[3]));
-    const int e15 = 15 - __builtin_amdgcn_frexp_expf(qm);  // the largest query in [2^14, 2^15)
-    if (tid < 4) s_scale[tid] = (float)e15;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int r = wave + 4 * i;
-      float sum = 0.0f;
+      for (int e = 0; e < D / 64; ++e) qm = fmaxf(qm, fabsf(x[e]));
+      qm = wave_max(qm);
+      const int e15 = 15 - __builtin_amdgcn_frexp_expf(qm);  // the row's largest in [2^14, 2^15)
 #pragma unroll
       for (int e = 0; e < D / 64; ++e) {
         const int d = lane * (D / 64) + e, f = d & 7;
-        const _Float16 h = (_Float16)__builtin_amdgcn_ldexpf(x[i][e], f & 1 ? e15 - 4 : e15);
+        const _Float16 h = (_Float16)__builtin_amdgcn_ldexpf(x[e], f & 1 ? e15 - 4 : e15);
         u.q[r][(d & ~7) + (f < 4 ? 2 * f : 2 * f - 7)] = h;
         sum += f & 1 ? 16.0f * (float)h : (float)h;
       }
       sum = wave_sum(sum);
-      if (lane == 0) s_qsum[r] = sum;
+      // scores in the log2 domain: dots carry 2^(e15 - 24), sums of q 2^e15
+      if (lane == 0) {
+        s_qsum[r] = __builtin_amdgcn_ldexpf(sum, -24);
+        s_slope[r] = __builtin_amdgcn_ldexpf(a.sm_scale * LOG2E, 24 - e15);
+      }
+    }
+    for (int i = 64 * wave + lane; i < (16 * RT - rows) * (D / 8); i += 256)
+      *reinterpret_cast<uint4*>(&u.q[rows + i / (D / 8)][i % (D / 8) * 8]) = make_uint4(0, 0, 0, 0);
+    if (tid >= rows && tid < 16 * RT) {
+      s_qsum[tid] = 0.0f;
+      s_slope[tid] = 1.0f;  // (finite and not 0: -inf at a masked position stays that)
     }
     __syncthreads();
   }
-  // scores in the log2 domain: dots carry 2^(e15 - 24), sums of q 2^e15
-  const int e15 = (int)s_scale[0];
-  const float slope = __builtin_amdgcn_ldexpf(a.sm_scale * LOG2E, 24 - e15);
   h8_t qb[RT][NW];
-  float qs[RT], m[RT], l[RT], zs[RT];
+  float qs[RT], slope[RT], m[RT], l[RT], zs[RT];
   int pos[RT];
   f4_t o[RT][NM];
 #pragma unroll
@@ -347,7 +316,8 @@ kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, 
 #pragma unroll
     for (int j = 0; j < NW; ++j)
       qb[t][j] = *reinterpret_cast<const h8_t*>(&u.q[16 * t + pr][kq * (D / 4) + 8 * j]);
-    qs[t] = __builtin_amdgcn_ldexpf(s_qsum[16 * t + pr], -24);
+    qs[t] = s_qsum[16 * t + pr];
+    slope[t] = s_slope[16 * t + pr];
     pos[t] = w.s.pos0 + (16 * t + pr) / G;
     m[t] = LOWEST;
     l[t] = zs[t] = 0.0f;
@@ -362,7 +332,7 @@ kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, 
     const int key = k0 + lane;
     const bool valid = lane < 32 && ((x.ok >> (lane >> 4)) & 1) && key < k_stop;
     const uint32_t vm = (uint32_t)__builtin_amdgcn_ballot_w64(valid);
-    const float sk = valid ? slope * fp16_bits_to_f32((uint16_t)x.par.x) : 0.0f;
+    const float sk = valid ? fp16_bits_to_f32((uint16_t)x.par.x) : 0.0f;
     const float zk = valid ? (float)(int16_t)(x.par.x >> 16) : 0.0f;
     const float sv = valid ? fp16_bits_to_f32((uint16_t)x.par.y) : 0.0f;
     const float zv = valid ? (float)(int16_t)(x.par.y >> 16) : 0.0f;
@@ -435,10 +405,10 @@ kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, 
 #pragma unroll
         for (int r = 0; r < 4; ++r) top = fmaxf(top, sc[g][r]);
       // The row's reference maximum moves only when a block passes it by more than TAU.
-      if (__builtin_amdgcn_ballot_w64(top > m[t] + TAU)) {
+      if (__builtin_amdgcn_ballot_w64(__builtin_fmaf(top, slope[t], -m[t]) > TAU)) {
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
-        const float mn = fmaxf(m[t], top);
+        const float mn = fmaxf(m[t], top * slope[t]);
         const float f = __builtin_amdgcn_exp2f(m[t] - mn);
         m[t] = mn;
         l[t] *= f;
@@ -452,8 +422,8 @@ kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, 
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float p0 = __builtin_amdgcn_exp2f(sc[i >> 1][2 * (i & 1)] - m[t]);
-        const float p1 = __builtin_amdgcn_exp2f(sc[i >> 1][2 * (i & 1) + 1] - m[t]);
+        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i >> 1][2 * (i & 1)], slope[t], -m[t]));
+        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i >> 1][2 * (i & 1) + 1], slope[t], -m[t]));
         l[t] += p0 + p1;
         const h2_t h = {(_Float16)(p0 * vp[i].x), (_Float16)(p1 * vp[i].z)};
         wb[t][i] = __builtin_bit_cast(uint32_t, h);
@@ -523,19 +493,25 @@ kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, 
   const float v_back = 1.0f / v_mul;
   for (int t = 0; t < RT; ++t) {
     if (16 * t >= rows) break;
+    if (16 * t + 4 * kq < rows) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int row = 16 * t + 4 * kq + r;
-      const float top = fmaxf(fmaxf(s_m[0][row], s_m[1][row]), fmaxf(s_m[2][row], s_m[3][row]));
-      const float f = __builtin_amdgcn_exp2f(s_m[wave][row] - top) * v_back, z = s_z[wave][row];
+      for (int r = 0; r < 4; ++r) {
+        const int row = 16 * t + 4 * kq + r;
+        const float top = fmaxf(fmaxf(s_m[0][row], s_m[1][row]), fmaxf(s_m[2][row], s_m[3][row]));
+        const float f = __builtin_amdgcn_exp2f(s_m[wave][row] - top) * v_back, z = s_z[wave][row];
+        float y[NM];
 #pragma unroll
-      for (int k = 0; k < NM; ++k) {
-        f4_t ov = o[0][k];
+        for (int k = 0; k < NM; ++k) {
+          f4_t ov = o[0][k];
 #pragma unroll
-        for (int tt = 1; tt < RT; ++tt)
-          if (tt == t) ov = o[tt][k];
-        u.o[wave][4 * kq + r][NM * pr + k] =
-            (__builtin_amdgcn_ldexpf(ov[r], k & 1 ? 20 : 24) - z) * f;
+          for (int tt = 1; tt < RT; ++tt)
+            if (tt == t) ov = o[tt][k];
+          y[k] = (__builtin_amdgcn_ldexpf(ov[r], k & 1 ? 20 : 24) - z) * f;
+        }
+#pragma unroll
+        for (int k = 0; k < NM; k += 4)
+          *reinterpret_cast<float4*>(&u.o[wave][4 * kq + r][NM * pr + k]) =
+              make_float4(y[k], y[k + 1], y[k + 2], y[k + 3]);
       }
     }
     __syncthreads();
@@ -687,23 +663,6 @@ __device__ __forceinline__ uint32_t pk_fma(uint32_t a, uint32_t b, uint32_t c) {
                                                       __builtin_bit_cast(h2_t, c)));
 }
 
-template <int CTRL>
-__device__ __forceinline__ float dpp(float x) {
-  return __builtin_bit_cast(
-      float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
-}
-// the wave's largest value (of values >= 0), the same in every lane
-__device__ __forceinline__ float wave_top(float v) {
-  v = fmaxf(v, dpp<0x128>(v));  // rotations within rows of 16 lanes
-  v = fmaxf(v, dpp<0x124>(v));
-  v = fmaxf(v, dpp<0x122>(v));
-  v = fmaxf(v, dpp<0x121>(v));
-  const int i = __builtin_bit_cast(int, v);
-  const int a = max(__builtin_amdgcn_readlane(i, 0), __builtin_amdgcn_readlane(i, 16));
-  const int b = max(__builtin_amdgcn_readlane(i, 32), __builtin_amdgcn_readlane(i, 48));
-  return __builtin_bit_cast(float, max(a, b));
-}
-
 // x = h1 + h2 + h3 + O(2^-33 x): fp16 pieces
 struct Pieces {
   float h1, h2, h3;
@@ -734,8 +693,7 @@ __device__ __forceinline__ Tile find_tile(const PagedAttentionArgs& a, int log2p
   };
   int count = 0, mine = 0;
   for (int b0 = 0; b0 < a.B; b0 += 64) count += mine = load(b0 + lane);
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) count += __shfl_xor(count, o);
+  count = wave_add(count);
   Tile r{};
   r.count = count;
   if (t >= count) return r;
@@ -743,12 +701,7 @@ __device__ __forceinline__ Tile find_tile(const PagedAttentionArgs& a, int log2p
   int base = 0;
   for (int b0 = 0; b0 < a.B; b0 += 64) {
     if (a.B > 64) mine = load(b0 + lane);
-    int incl = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int p = __shfl_up(incl, o);
-      if (lane >= o) incl += p;
-    }
+    const int incl = wave_scan(mine);
     const int first = base + incl - mine;
     const uint64_t hit = __builtin_amdgcn_ballot_w64(r.index >= first && r.index < first + mine);
     if (hit) {
@@ -902,14 +855,14 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
     const float sk = fp16_bits_to_f32((uint16_t)p.x), zk = (float)(int16_t)(p.x >> 16);
     const float sv = fp16_bits_to_f32((uint16_t)p.y), zv = (float)(int16_t)(p.y >> 16);
     // keys: A (8192 + |z|) stays below 2^28: A below 2^15, the pieces of A z 2^-13 as well
-    const float kt = wave_top(sk * (8192.0f + fabsf(zk)));
+    const float kt = wave_max(sk * (8192.0f + fabsf(zk)));
     if (__builtin_amdgcn_ldexpf(kt, -E) >= 0x1p28f) E = __builtin_amdgcn_frexp_expf(kt) - 25;
     const float ka = __builtin_amdgcn_ldexpf(sk, -E);
     const Pieces u = pieces(ka * zk * 0x1p-13f);
     P.z[lane] = make_uint4(pk_f16(u.h1, u.h1), pk_f16(u.h2, u.h1), pk_f16(u.h2, u.h3), 0);
     P.a[lane] = pk_f16(ka, ka * 0.0625f);
     // values: A (16 + |z|) stays below 2^19
-    const float vt = wave_top(sv * (16.0f + fabsf(zv)));
+    const float vt = wave_max(sv * (16.0f + fabsf(zv)));
     if (vt > 0.0f) F = max(F, __builtin_amdgcn_frexp_expf(vt) - 19);
     const float va = __builtin_amdgcn_ldexpf(sv, -F);
     P.ab[lane] = pk_f16(va, -va * zv * 0x1p-9f);
@@ -971,18 +924,15 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
             x[i + s] = p - q;
           }
 #pragma unroll
-      for (int i = 0; i < D / 2; ++i) {
-        const float p = __shfl_xor(x[i], 32);
-        x[i] = hadamard_norm<D>() * (h ? p - x[i] : x[i] + p);
-      }
+      for (int i = 0; i < D / 2; ++i) x[i] = hadamard_norm<D>() * lane_butterfly<32>(x[i], lane);
     }
     // E: the largest query at 2^4 at most, unless the first block's keys would leave their range
     float qm = 0.0f;
 #pragma unroll
     for (int i = 0; i < D / 2; ++i) qm = fmaxf(qm, fabsf(x[i]));
-    qm = wave_top(qm);
+    qm = wave_max(qm);
     const float sm2 = a.sm_scale * LOG2E;
-    const float kt = wave_top(any && (uint32_t)fpage[0] < (uint32_t)c.pages &&
+    const float kt = wave_max(any && (uint32_t)fpage[0] < (uint32_t)c.pages &&
                                           kb0 * KB + lane < keys
                                       ? fp16_bits_to_f32((uint16_t)fpar[0].x) *
                                         (8192.0f + fabsf((float)(int16_t)(fpar[0].x >> 16)))
@@ -1223,10 +1173,8 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
           o[(i + s) >> 4][(i + s) & 15] = p - q;
         }
 #pragma unroll
-    for (int i = 0; i < D / 2; ++i) {
-      const float x = o[i >> 4][i & 15], p = __shfl_xor(x, 32);
-      o[i >> 4][i & 15] = hadamard_norm<D>() * (h ? p - x : x + p);
-    }
+    for (int i = 0; i < D / 2; ++i)
+      o[i >> 4][i & 15] = hadamard_norm<D>() * lane_butterfly<32>(o[i >> 4][i & 15], lane);
   }
   if (!mine) return;
   uint16_t* dst = a.out + (int64_t)(w.s.q0 + tok) * a.ldo + (int64_t)hq * D;
@@ -1281,10 +1229,15 @@ struct Shape {
   int64_t tiles;
   int splits;
 };
-Shape attention_shape(int64_t M, int64_t B, int64_t Hq, int64_t Hkv, int64_t max_new, int64_t cap) {
+Shape attention_shape(int64_t M, int64_t B, int64_t Hq, int64_t Hkv, int D, int64_t max_new,
+                    int64_t cap) {
   const int64_t G = Hq / Hkv, most = max_new * G;
   Shape f = {};
-  f.many = most > 64;
+  // The few-row kernel reads each code once into its operands, which costs the least per position,
+  // but its time grows with the row tiles, and at 64 rows of 128 channels it runs out of
+  // registers: 8 new tokens of 8 heads, 4 x 5000 positions: 92 us here, 55 us as a tile that is
+  // three quarters empty (5 tokens: 82, 47).  At 64 channels 32 us here, 51 us as a tile.
+  f.many = most > (D == 128 ? 32 : 64);
   f.few = !f.many || B > 1;  // a single sequence of many rows: one launch
   f.row_tiles = f.many || most <= 16 ? 1 : most <= 32 ? 2 : 4;
   f.few_rows = f.few ? (int)(f.many ? 16 : most) : 0;
@@ -1316,13 +1269,13 @@ int64_t tile_floats(const Shape& f, int64_t Hkv, int D) {
 
 int64_t kv_attention_paged_workspace_floats(int64_t M, int64_t B, int64_t Hq, int64_t Hkv,
                                             int head_dim, int64_t max_new) {
-  const Shape f = attention_shape(M, B, Hq, Hkv, max_new, int64_t(1) << 30);
+  const Shape f = attention_shape(M, B, Hq, Hkv, head_dim, max_new, int64_t(1) << 30);
   return (few_floats(f, B, head_dim) + 3) / 4 * 4 + tile_floats(f, Hkv, head_dim);
 }
 
 hipError_t launch_kv_attention_paged(const PagedAttentionArgs& a, const PagedCache& c, int head_dim,
                                      float* workspace, hipStream_t stream) {
-  const Shape f = attention_shape(a.M, a.B, a.Hq, c.Hkv, a.max_new, (int64_t)a.max_pages << c.log2p);
+  const Shape f = attention_shape(a.M, a.B, a.Hq, c.Hkv, head_dim, a.max_new, (int64_t)a.max_pages << c.log2p);
   if (f.few) {
     Joint* joints = f.few_join ? reinterpret_cast<Joint*>(workspace) : nullptr;
     float* rec = workspace + 4 * (int64_t)a.B;
@@ -1331,8 +1284,7 @@ hipError_t launch_kv_attention_paged(const PagedAttentionArgs& a, const PagedCac
                      0, stream, a, c, f.few_rows, f.slots, joints, rec)
     if (head_dim == 128) {
       if (f.row_tiles == 1) OFFQ_FEW(128, 1);
-      else if (f.row_tiles == 2) OFFQ_FEW(128, 2);
-      else OFFQ_FEW(128, 4);
+      else OFFQ_FEW(128, 2);
     } else {
       if (f.row_tiles == 1) OFFQ_FEW(64, 1);
       else if (f.row_tiles == 2) OFFQ_FEW(64, 2);
