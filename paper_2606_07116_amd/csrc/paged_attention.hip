@@ -727,7 +727,7 @@ struct alignas(16) TileJoint {
 
 template <int D>
 __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
-    PagedAttentionArgs a, PagedCache c, int few_rows, int splits, TileJoint* __restrict__ joints,
+    PagedAttentionArgs a, PagedCache c, int few_rows, int tiles, int splits, TileJoint* __restrict__ joints,
     float* __restrict__ rec) {
   constexpr int KROW = 2 * D + 16;
   constexpr int NS = D / 16;   // k-steps of the score product
@@ -740,8 +740,11 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
   const int ql = lane & 31, h = lane >> 5;
   const int G = a.Hq / c.Hkv;
   const int id = (int)__builtin_amdgcn_workgroup_id_x();
-  const int split = uniform(id % splits), hk = uniform(id / splits % c.Hkv);
-  const int t = uniform(id / splits / c.Hkv);
+  // (heads first: an L2 reads one head's cache when there are eight.  Splits last: those that a
+  // short tile does without end at once, and are not every n-th workgroup, which would leave
+  // whole XCDs idle)
+  const int hk = uniform(id % c.Hkv), t = uniform(id / c.Hkv % tiles);
+  const int split = uniform(id / c.Hkv / tiles);
   const Tile w = find_tile(a, c.log2p, G, few_rows, t);
   if (!w.found) {
     if (joints && !split && !hk && !tid) joints[t] = TileJoint{0, 0, 0, 0};
@@ -752,6 +755,7 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
   // the positions that its rows see, and this split's blocks of them
   const int keys = uniform(min(max(w.s.pos0 + last / G + 1, 0), w.s.keys));
   const int nblk = (keys + KB - 1) / KB;
+  // (four blocks a split at least: 700 new tokens 36 us, with eight 39)
   const int ns = max(1, min(splits, nblk / 4));
   if (joints && !split && !hk && !tid) joints[w.index] = TileJoint{w.s.q0, row0, last + 1 - row0, ns};
   if (split >= ns) return;
@@ -1246,8 +1250,8 @@ Shape attention_shape(int64_t M, int64_t B, int64_t Hq, int64_t Hkv, int D, int6
   f.units = (int)((f.few_join ? 2 * f.slots : 0) + B * Hkv);
   f.splits = 1;
   if (f.many) {
-    // (a sequence adds at most one tile that is not full)
-    f.tiles = M * G / ROWS + (B < M ? B : M);
+    // (a sequence of r rows has ceil(r / ROWS) tiles)
+    f.tiles = (M * G + (ROWS - 1) * (B < M ? B : M)) / ROWS;
     const int64_t wgs = f.tiles * Hkv;
     // one workgroup per CU: the fewest splits that keep nine in ten of 256 CUs busy
     for (int s = 1; s <= 64 && wgs * s <= 768; ++s) {
@@ -1304,7 +1308,7 @@ hipError_t launch_kv_attention_paged(const PagedAttentionArgs& a, const PagedCac
     const dim3 grid((unsigned)(f.tiles * c.Hkv * f.splits));
     hipLaunchKernelGGL(head_dim == 128 ? kv_attention_paged_tile_kernel<128>
                                        : kv_attention_paged_tile_kernel<64>,
-                       grid, dim3(512), 0, stream, a, c, f.few_rows, f.splits, joints, rec);
+                       grid, dim3(512), 0, stream, a, c, f.few_rows, (int)f.tiles, f.splits, joints, rec);
     if (f.splits > 1)
       hipLaunchKernelGGL(head_dim == 128 ? kv_attention_paged_tile_join_kernel<128>
                                          : kv_attention_paged_tile_join_kernel<64>,
