@@ -18,6 +18,7 @@ constexpr int CHUNK_MIN = 512;   // positions of a chunk, at least
 
 typedef _Float16 h8_t __attribute__((ext_vector_type(8)));
 typedef _Float16 h2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 b8_t __attribute__((ext_vector_type(8)));
 typedef float f4_t __attribute__((ext_vector_type(4)));
 
 constexpr float TAU = 8.0f;     // a row's reference maximum may lag by up to 2^TAU
@@ -768,6 +769,11 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
   const int tok = row / G, hq = hk * G + row - tok * G;
   const int pos = w.s.pos0 + tok;
   const int pmin = uniform(w.s.pos0 + wrow / G);
+  uint4 raw[NS];
+#pragma unroll
+  for (int s = 0; s < NS; ++s)
+    raw[s] = *reinterpret_cast<const uint4*>(a.q + (int64_t)(w.s.q0 + tok) * a.ldq + (int64_t)hq * D +
+                                             16 * s + 8 * h);
 
   // ---- staging: eight positions a wave; a block's parameters are prepared by one wave, in turn
   const int32_t* table = a.page_table + (int64_t)w.b * a.max_pages;
@@ -900,64 +906,68 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
     for (int i = 0; i < 3; ++i) fpar[i] = params(kb0 + i, fpage[i]);
   }
 
-  // ---- queries: channels D / 2 h .. of the row, rotated, times sm_scale log2(e) 2^(E + 9)
+  // ---- queries, rotated, times sm_scale log2(e) 2^(E + 9).  32 channels at a time are rotated by
+  // a matrix product with H (its entries and the queries are exact, the sums fp32), whose rows
+  // stand in such an order that half h of the lanes gets channels 16 h .. 16 h + 15 of the 32, two
+  // code words; without a rotation the product is with 1.
   uint32_t qb[NS][4], zb[4] = {0, 0, 0, 0};
   int E;
   {
-    float x[D / 2];
-    const uint4* src = reinterpret_cast<const uint4*>(a.q + (int64_t)(w.s.q0 + tok) * a.ldq +
-                                                      (int64_t)hq * D + D / 2 * h);
+    const int ch = 16 * ((ql >> 2) & 1) + 4 * (ql >> 3) + (ql & 3);
+    auto entry = [&](int k) {
+      return a.k_had ? 0x3F80u | ((uint32_t)__builtin_popcount(ch & k) << 15 & 0x8000u)
+                     : (ch == k ? 0x3F80u : 0u);
+    };
+    uint32_t rot[2][4];
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) {
-      const uint4 v = src[i];
-      const uint32_t y[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        x[8 * i + 2 * k] = bf16_lo(y[k]);
-        x[8 * i + 2 * k + 1] = bf16_hi(y[k]);
-      }
+    for (int k = 0; k < 8; ++k) {
+      const int i = 16 * (k >> 2) + 8 * h + 2 * (k & 3);
+      rot[k >> 2][k & 3] = entry(i) | entry(i + 1) << 16;
     }
+    f16_t x[ND];
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[d][r] = 0.0f;
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        x[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            __builtin_bit_cast(b8_t, make_uint4(rot[k][0], rot[k][1], rot[k][2], rot[k][3])),
+            __builtin_bit_cast(b8_t, raw[2 * d + k]), x[d], 0, 0, 0);
+    }
+    float sm2 = a.sm_scale * LOG2E;
     if (a.k_had) {
 #pragma unroll
-      for (int s = 1; s < D / 2; s <<= 1)
+      for (int s = 1; s < ND; s <<= 1)
 #pragma unroll
-        for (int i = 0; i < D / 2; ++i)
-          if (!(i & s)) {
-            const float p = x[i], q = x[i + s];
-            x[i] = p + q;
-            x[i + s] = p - q;
+        for (int d = 0; d < ND; ++d)
+          if (!(d & s)) {
+            const f16_t p = x[d], q = x[d + s];
+            x[d] = p + q;
+            x[d + s] = p - q;
           }
-#pragma unroll
-      for (int i = 0; i < D / 2; ++i) x[i] = hadamard_norm<D>() * lane_butterfly<32>(x[i], lane);
+      sm2 *= hadamard_norm<D>();
     }
-    // E: the largest query at 2^4 at most, unless the first block's keys would leave their range
+    // E: the largest query at 2^4 at most (a block whose keys would leave their range raises it)
     float qm = 0.0f;
 #pragma unroll
-    for (int i = 0; i < D / 2; ++i) qm = fmaxf(qm, fabsf(x[i]));
+    for (int i = 0; i < D / 2; ++i) qm = fmaxf(qm, fabsf(x[i >> 4][i & 15]));
     qm = wave_max(qm);
-    const float sm2 = a.sm_scale * LOG2E;
-    const float kt = wave_max(any && (uint32_t)fpage[0] < (uint32_t)c.pages &&
-                                          kb0 * KB + lane < keys
-                                      ? fp16_bits_to_f32((uint16_t)fpar[0].x) *
-                                        (8192.0f + fabsf((float)(int16_t)(fpar[0].x >> 16)))
-                                  : 0.0f);
     if (lane == 0) s_qm[wave] = qm;
     __syncthreads();
     qm = s_qm[0];
 #pragma unroll
     for (int k = 1; k < 8; ++k) qm = fmaxf(qm, s_qm[k]);
-    E = uniform(-5 - __builtin_amdgcn_frexp_expf(qm) - __builtin_amdgcn_frexp_expf(sm2));
-    if (kt > 0.0f) E = max(E, uniform(__builtin_amdgcn_frexp_expf(kt)) - 25);
+    E = uniform(-5 - max(__builtin_amdgcn_frexp_expf(qm), -100) - __builtin_amdgcn_frexp_expf(sm2));
+    const float f = __builtin_amdgcn_ldexpf(sm2, E + 9);
     float sum = 0.0f;
 #pragma unroll
     for (int s = 0; s < NS; ++s)
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const float lo = __builtin_amdgcn_ldexpf(sm2 * x[8 * s + k], E + 9);
-        const float hi = __builtin_amdgcn_ldexpf(sm2 * x[8 * s + k + 4], E + 9);
-        const h2_t p = {(_Float16)__builtin_amdgcn_fmed3f(lo, -65504.0f, 65504.0f),
-                        (_Float16)__builtin_amdgcn_fmed3f(hi, -65504.0f, 65504.0f)};
-        sum += (float)p.x + (float)p.y;
+        const h2_t p = {(_Float16)(f * x[s >> 1][8 * (s & 1) + k]),
+                        (_Float16)(f * x[s >> 1][8 * (s & 1) + k + 4])};
+        sum = __builtin_amdgcn_fdot2(p, h2_t{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
         qb[s][k] = __builtin_bit_cast(uint32_t, p);
       }
     sum += __shfl_xor(sum, 32);
@@ -987,7 +997,8 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
         __builtin_bit_cast(h8_t, make_uint4(zb[0], zb[1], zb[2], zb[3])), neg, 0, 0, 0);
 #pragma unroll
     for (int k = 0; k < NS; ++k) {
-      const uint4 kk = *reinterpret_cast<const uint4*>(S.k[slot] + (32 * tt + ql) * KROW + D * h + 16 * k);
+      const uint4 kk = *reinterpret_cast<const uint4*>(S.k[slot] + (32 * tt + ql) * KROW + 64 * (k >> 1) +
+                                                       32 * h + 16 * (k & 1));
       s = __builtin_amdgcn_mfma_f32_32x32x16_f16(
           __builtin_bit_cast(h8_t, kk),
           __builtin_bit_cast(h8_t, make_uint4(qb[k][0], qb[k][1], qb[k][2], qb[k][3])), s, 0, 0, 0);
