@@ -14,7 +14,10 @@ namespace offq {
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr int CHUNK_MIN = 512;   // positions of a chunk, at least
+// Positions of a chunk, at least: of one that is joined, and where no sequence is longer.  (A chunk
+// that is joined at all may as well be short: one token after 4 x 2000 positions 12.9 us, with 512
+// 14.2; one after 300 in a cache of 304: 12.2 us with 256 and the join, 9.9 without.)
+constexpr int CHUNK_MIN = 256, CHUNK_ONE = 512;
 
 typedef _Float16 h8_t __attribute__((ext_vector_type(8)));
 typedef _Float16 h2_t __attribute__((ext_vector_type(2)));
@@ -77,7 +80,7 @@ struct Chunking {
 // mean in several rounds.  The cost of a unit besides its positions is that of about 400 (6 us).
 // Every wave works it out for itself, 64 sequences at a time.
 __device__ __forceinline__ Chunking find_chunk(const PagedAttentionArgs& a, int log2p, int Hkv,
-                                               int few_rows, int slots, int unit) {
+                                               int few_rows, int slots, int chunk_min, int unit) {
   const int lane = (int)__builtin_amdgcn_workitem_id_x() & 63;
   const int G = a.Hq / Hkv;
   Seq s{};
@@ -101,7 +104,7 @@ __device__ __forceinline__ Chunking find_chunk(const PagedAttentionArgs& a, int 
     total += wave_add(s.rows ? (s.keys + 127) >> 7 : 0);
   }
   const int mean = uniform((int)min((total * Hkv * 128 + slots - 1) / slots, (int64_t)1 << 30));
-  auto round_up = [](int64_t v) { return (int)max((int64_t)CHUNK_MIN, (v + 127) & ~(int64_t)127); };
+  auto round_up = [&](int64_t v) { return (int)max((int64_t)chunk_min, (v + 127) & ~(int64_t)127); };
   const int several = round_up((mean + 1) / 2);  // at most 2 slots + a unit per sequence and head
   Chunking c{};
   c.len = round_up(mean);
@@ -206,7 +209,8 @@ kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, 
   const int pr = lane & 15, kq = lane >> 4;
   const int unit = (int)__builtin_amdgcn_workgroup_id_x();
   const int G = a.Hq / c.Hkv;
-  const Chunking w = find_chunk(a, c.log2p, c.Hkv, few_rows, slots, unit);
+  const Chunking w = find_chunk(a, c.log2p, c.Hkv, few_rows, slots,
+                                joints ? CHUNK_MIN : CHUNK_ONE, unit);
   if (!w.found) return;
   const int rows = w.s.rows, hk = w.head;
   if (joints && w.chunk == 0 && hk == 0 && tid == 0)
@@ -769,11 +773,6 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
   const int tok = row / G, hq = hk * G + row - tok * G;
   const int pos = w.s.pos0 + tok;
   const int pmin = uniform(w.s.pos0 + wrow / G);
-  uint4 raw[NS];
-#pragma unroll
-  for (int s = 0; s < NS; ++s)
-    raw[s] = *reinterpret_cast<const uint4*>(a.q + (int64_t)(w.s.q0 + tok) * a.ldq + (int64_t)hq * D +
-                                             16 * s + 8 * h);
 
   // ---- staging: eight positions a wave; a block's parameters are prepared by one wave, in turn
   const int32_t* table = a.page_table + (int64_t)w.b * a.max_pages;
@@ -899,6 +898,18 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
     for (int i = 0; i < 3; ++i) fpage[i] = page_of(kb0 + i);
     find_pages(kpg, kb0 * KB);
     vpg = kpg;
+  }
+  // the wave's query rows, whole rows at a time, and through LDS to the lanes that want them
+  // (a lane that reads its row itself: 32 bytes of a line at a time, 0.3 us more)
+  uint4 raw[NS];
+  constexpr int LR = D / 8;  // lanes that read a row
+#pragma unroll
+  for (int s = 0; s < NS; ++s) {
+    const int i = 64 / LR * s + lane / LR, r = min(wrow + i, last);
+    raw[s] = *reinterpret_cast<const uint4*>(a.q + w.s.q0 * a.ldq + (int64_t)hk * G * D + (int64_t)r * D +
+                                             __shfl(tok, i) * (a.ldq - G * D) + 8 * (lane % LR));
+  }
+  if (any) {
     load_k(kb0);
     load_v(kb0);
     par0 = params(kb0 + 3 + wave, page0);
@@ -924,6 +935,15 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
       const int i = 16 * (k >> 2) + 8 * h + 2 * (k & 3);
       rot[k >> 2][k & 3] = entry(i) | entry(i + 1) << 16;
     }
+    static_assert(8 * 32 * KROW <= sizeof(S.k) + sizeof(S.v), "");
+    uint8_t* own = &S.k[0][0] + 32 * KROW * wave;
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+      *reinterpret_cast<uint4*>(own + (64 / LR * s + lane / LR) * KROW + 16 * (lane % LR)) = raw[s];
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+      raw[s] = *reinterpret_cast<const uint4*>(own + ql * KROW + 32 * s + 16 * h);
     f16_t x[ND];
 #pragma unroll
     for (int d = 0; d < ND; ++d) {
@@ -1248,16 +1268,17 @@ Shape attention_shape(int64_t M, int64_t B, int64_t Hq, int64_t Hkv, int D, int6
                     int64_t cap) {
   const int64_t G = Hq / Hkv, most = max_new * G;
   Shape f = {};
-  // The few-row kernel reads each code once into its operands, which costs the least per position,
+  // The few-row kernel takes codes straight into its operands, which costs the least per position,
   // but its time grows with the row tiles, and at 64 rows of 128 channels it runs out of
-  // registers: 8 new tokens of 8 heads, 4 x 5000 positions: 92 us here, 55 us as a tile that is
-  // three quarters empty (5 tokens: 82, 47).  At 64 channels 32 us here, 51 us as a tile.
-  f.many = most > (D == 128 ? 32 : 64);
+  // registers: 8 new tokens of 8 heads, 4 x 5000 positions: 92 us there, 46 us as a tile that is
+  // three quarters empty; 5 tokens: 46 both, 334 and 377 us with 64 x 5000.  64 rows of 64
+  // channels: 32 us there, 51 us as a tile.
+  f.many = most > (D == 128 ? 48 : 64);
   f.few = !f.many || B > 1;  // a single sequence of many rows: one launch
-  f.row_tiles = f.many || most <= 16 ? 1 : most <= 32 ? 2 : 4;
+  f.row_tiles = f.many || most <= 16 ? 1 : most <= 32 ? 2 : most <= 48 ? 3 : 4;
   f.few_rows = f.few ? (int)(f.many ? 16 : most) : 0;
   f.slots = 512;  // two workgroups a CU
-  f.few_join = f.few && cap > CHUNK_MIN;
+  f.few_join = f.few && cap > CHUNK_ONE;
   f.units = (int)((f.few_join ? 2 * f.slots : 0) + B * Hkv);
   f.splits = 1;
   if (f.many) {
@@ -1299,10 +1320,12 @@ hipError_t launch_kv_attention_paged(const PagedAttentionArgs& a, const PagedCac
                      0, stream, a, c, f.few_rows, f.slots, joints, rec)
     if (head_dim == 128) {
       if (f.row_tiles == 1) OFFQ_FEW(128, 1);
-      else OFFQ_FEW(128, 2);
+      else if (f.row_tiles == 2) OFFQ_FEW(128, 2);
+      else OFFQ_FEW(128, 3);
     } else {
       if (f.row_tiles == 1) OFFQ_FEW(64, 1);
       else if (f.row_tiles == 2) OFFQ_FEW(64, 2);
+      else if (f.row_tiles == 3) OFFQ_FEW(64, 3);
       else OFFQ_FEW(64, 4);
     }
 #undef OFFQ_FEW
