@@ -28,9 +28,14 @@ __device__ __forceinline__ void load8(const uint16_t* p, float* x) {
   }
 }
 
+typedef uint32_t u4_t __attribute__((ext_vector_type(4)));
+
+template <bool NT>  // past the caches
 __device__ __forceinline__ void store8(uint16_t* p, const float* x) {
-  *reinterpret_cast<uint4*>(p) = make_uint4(bf16x2_rne(x[0], x[1]), bf16x2_rne(x[2], x[3]),
-                                            bf16x2_rne(x[4], x[5]), bf16x2_rne(x[6], x[7]));
+  const u4_t v = {bf16x2_rne(x[0], x[1]), bf16x2_rne(x[2], x[3]), bf16x2_rne(x[4], x[5]),
+                  bf16x2_rne(x[6], x[7])};
+  if constexpr (NT) __builtin_nontemporal_store(v, reinterpret_cast<u4_t*>(p));
+  else *reinterpret_cast<u4_t*>(p) = v;
 }
 
 // amplitude * (cos, sin) of pos * f
@@ -67,7 +72,8 @@ __device__ __forceinline__ uint32_t quantize_row(const float* x, uint32_t& par) 
 // lanes each.  The token's angles are formed by the wave, one pair a lane, and handed round in
 // LDS; the next units' channels are on their way while one is worked on.
 // FULL: the half layout over the whole head, whose partner channels sit half a group away.
-template <int D, bool FULL>
+// NT: what is read and the queries written go past the caches.
+template <int D, bool FULL, bool NT>
 __global__ __launch_bounds__(256) void rope_kv_paged_kernel(RopeKvPagedArgs a, PagedCache c, int parts) {
   constexpr int LPH = D / 8, NG = 64 / LPH;
   __shared__ alignas(16) float2 s_cs[4][D / 2];
@@ -80,11 +86,14 @@ __global__ __launch_bounds__(256) void rope_kv_paged_kernel(RopeKvPagedArgs a, P
   const int l = lane & (LPH - 1), g = lane / LPH;
   const int units = a.Hq + c.Hkv;
   const uint16_t* row = a.qkv + m * a.ldq + 8 * l;
-  uint4 next, vnext = make_uint4(0, 0, 0, 0);
+  u4_t next, vnext = {0, 0, 0, 0};
+  auto load = [&](int unit) {
+    const u4_t* p = reinterpret_cast<const u4_t*>(row + (int64_t)unit * D);
+    return NT ? __builtin_nontemporal_load(p) : *p;
+  };
   auto fetch = [&](int j) {  // channels of unit j: a query's, or a key's and its value's
-    next = *reinterpret_cast<const uint4*>(row + (int64_t)min(j, units - 1) * D);
-    if (j >= a.Hq)
-      vnext = *reinterpret_cast<const uint4*>(row + (int64_t)min(j + c.Hkv, units + c.Hkv - 1) * D);
+    next = load(min(j, units - 1));
+    if (j >= a.Hq) vnext = load(min(j + c.Hkv, units + c.Hkv - 1));
   };
   int j = part * NG + g;
   const int step = parts * NG;
@@ -134,12 +143,11 @@ __global__ __launch_bounds__(256) void rope_kv_paged_kernel(RopeKvPagedArgs a, P
       }
     }
   };
-  auto unpack = [](const uint4& v, float* x) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  auto unpack = [](const u4_t& v, float* x) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      x[2 * k] = bf16_lo(w[k]);
-      x[2 * k + 1] = bf16_hi(w[k]);
+      x[2 * k] = bf16_lo(v[k]);
+      x[2 * k + 1] = bf16_hi(v[k]);
     }
   };
   auto rotate = [&](float* x) {
@@ -154,7 +162,7 @@ __global__ __launch_bounds__(256) void rope_kv_paged_kernel(RopeKvPagedArgs a, P
     fetch(j + step);
     if (j < a.Hq) {
       prepared(x, a.q_weight, qw);
-      store8(a.q_out + m * a.ldo + (int64_t)j * D + 8 * l, x);
+      store8<NT>(a.q_out + m * a.ldo + (int64_t)j * D + 8 * l, x);
     } else if (j < units) {
       uint32_t kp, vp;
       prepared(x, a.k_weight, kw);
@@ -221,17 +229,9 @@ __device__ __forceinline__ void dequantize_row(uint32_t w, uint32_t par, int l, 
     y[i + 4] = __builtin_fmaf((float)h[i].y, kk, sub);
   }
   if (HAD && l == 0) y[0] = __builtin_fmaf((float)h[0].x, 0x1p24f, -z * D) * k;
-  if constexpr (NT) {
-    typedef uint32_t u4_t __attribute__((ext_vector_type(4)));
-    const u4_t v = {bf16x2_rne(y[0], y[1]), bf16x2_rne(y[2], y[3]), bf16x2_rne(y[4], y[5]),
-                    bf16x2_rne(y[6], y[7])};
-    __builtin_nontemporal_store(v, reinterpret_cast<u4_t*>(out));
-  } else {
-    store8(out, y);
-  }
+  store8<NT>(out, y);
 }
 
-// NT: non-temporal stores.
 template <int D, bool NT>
 __global__ __launch_bounds__(256) void kv_dequantize_paged_kernel(
     PagedCache c, const int64_t* __restrict__ slots, int64_t M, int k_had, int v_had,
@@ -271,8 +271,13 @@ hipError_t launch_rope_kv_paged(const RopeKvPagedArgs& a, const PagedCache& c, i
   parts = parts < 1 ? 1 : parts > rounds ? rounds : parts;
   const dim3 grid((unsigned)((a.M * parts + 3) / 4));
   const bool full = !a.pairs && a.rotary == head_dim;
-#define OFFQ_ROPE(D_, F_) \
-  hipLaunchKernelGGL((rope_kv_paged_kernel<D_, F_>), grid, dim3(256), 0, stream, a, c, (int)parts)
+  // Queries beyond the L2s' 32 MB, and what they come from, bypass the caches (8191 tokens of 48
+  // heads: 47 -> 42 us); with 24 MB of input that costs more than it gives (2000 tokens of 48 heads
+  // with their reading back: 17.5 us, bypassing 19.6).
+  const bool nt = 2 * a.M * a.Hq * head_dim > (32 << 20);
+#define OFFQ_ROPE(D_, F_)                                                                        \
+  hipLaunchKernelGGL((nt ? rope_kv_paged_kernel<D_, F_, true> : rope_kv_paged_kernel<D_, F_, false>), \
+                     grid, dim3(256), 0, stream, a, c, (int)parts)
   if (head_dim == 128) {
     if (full) OFFQ_ROPE(128, true);
     else OFFQ_ROPE(128, false);
