@@ -501,8 +501,8 @@ offq_status_t offq_rope_kv_paged(const uint16_t* qkv, int64_t ldq, int64_t M, in
   if (M < 0 || Hq <= 0) return fail(OFFQ_ERR_INVALID, "need M >= 0, Hq > 0");
   if (offq_status_t st = check_paged(Hkv, head_dim, num_pages, page_size, k_hadamard, v_hadamard))
     return st;
-  if (Hq > (1 << 16) || M > (int64_t(1) << 31) - 1 || ldq > (int64_t(1) << 40) ||
-      ldo > (int64_t(1) << 40))
+  // (a launch has less than 2^32 threads: a wave per token, head_dim / 8 lanes per row read back)
+  if (Hq > (1 << 16) || M > (1 << 26) - 4 || ldq > (int64_t(1) << 40) || ldo > (int64_t(1) << 40))
     return fail(OFFQ_ERR_UNSUPPORTED, "sizes too large");
   if (ldq < (Hq + 2 * Hkv) * head_dim || ldq % 8 || ldo < Hq * head_dim || ldo % 8)
     return fail(OFFQ_ERR_INVALID,
@@ -543,7 +543,7 @@ offq_status_t offq_kv_dequantize_paged(const uint8_t* k_codes, const uint8_t* v_
   if (M < 0) return fail(OFFQ_ERR_INVALID, "need M >= 0");
   if (offq_status_t st = check_paged(Hkv, head_dim, num_pages, page_size, k_hadamard, v_hadamard))
     return st;
-  if (M > (int64_t(1) << 31) - 1 || M * Hkv > (int64_t(1) << 34) || ldk > (int64_t(1) << 40) ||
+  if (M >= (1 << 28) || M * Hkv * head_dim >= (int64_t(1) << 35) - 4096 || ldk > (int64_t(1) << 40) ||
       ldv > (int64_t(1) << 40))
     return fail(OFFQ_ERR_UNSUPPORTED, "sizes too large");
   if ((k_out && (ldk < Hkv * head_dim || ldk % 8)) || (v_out && (ldv < Hkv * head_dim || ldv % 8)))
@@ -577,7 +577,7 @@ bool paged_attention_sizes(int64_t M, int64_t B, int64_t Hq, int64_t Hkv, int32_
                            int64_t max_new) {
   return M >= 0 && B >= 0 && max_new >= 0 && Hq > 0 && Hkv > 0 && Hq % Hkv == 0 &&
          (head_dim == 64 || head_dim == 128) && M <= (1 << 24) && B <= (1 << 20) &&
-         Hq <= (1 << 12) && M * Hq <= (int64_t(1) << 30) && B * Hkv <= (1 << 22);
+         Hq <= (1 << 12) && M * Hq <= (int64_t(1) << 30) && B * Hkv < (1 << 18);
 }
 }  // namespace
 

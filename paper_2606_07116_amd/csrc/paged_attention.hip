@@ -74,77 +74,93 @@ struct Chunking {
   Seq s;
 };
 
-// The chunk length, and what unit `unit` is.  `slots` workgroups are resident at once.  One round
-// of units costs its longest chunk, so the shortest length whose units fit the slots is tried
-// first; where it is far above the mean (a few long sequences among many), chunks of half the
-// mean in several rounds.  The cost of a unit besides its positions is that of about 400 (6 us).
-// Every wave works it out for itself, 64 sequences at a time.
-__device__ __forceinline__ Chunking find_chunk(const PagedAttentionArgs& a, int log2p, int Hkv,
-                                               int few_rows, int slots, int chunk_min, int unit) {
-  const int lane = (int)__builtin_amdgcn_workitem_id_x() & 63;
-  const int G = a.Hq / Hkv;
-  Seq s{};
-  auto load = [&](int b) {
-    s = Seq{};
-    if (b < a.B) s = sequence(a, log2p, G, b);
-    if (s.rows > few_rows) s.rows = 0;
-  };
-  auto chunks = [&](int len) { return s.rows ? max(1, (s.keys + len - 1) / len) : 0; };
-  auto units = [&](int len) {
-    int n = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 64) {
-      if (a.B > 64) load(b0 + lane);
-      n += chunks(len);
-    }
-    return (int64_t)Hkv * wave_add(n);
-  };
-  int64_t total = 0;  // in blocks of 128
-  for (int b0 = 0; b0 < a.B; b0 += 64) {
-    load(b0 + lane);
-    total += wave_add(s.rows ? (s.keys + 127) >> 7 : 0);
-  }
-  const int mean = uniform((int)min((total * Hkv * 128 + slots - 1) / slots, (int64_t)1 << 30));
+// The chunk length.  `slots` workgroups are resident at once.  One round of units costs its longest
+// chunk, so the shortest length whose units fit the slots is tried first; where it is far above
+// the mean (a few long sequences among many), or there are more sequences than slots, chunks of
+// half the mean in several rounds.  The cost of a unit besides its positions is that of about 400
+// (6 us).  `blocks` of 128 positions; units(len): how many units that gives.
+template <typename Units>
+__device__ __forceinline__ int chunk_length(int64_t blocks, int Hkv, int slots, int chunk_min, Units units) {
+  const int mean = uniform((int)min((blocks * Hkv * 128 + slots - 1) / slots, (int64_t)1 << 30));
   auto round_up = [&](int64_t v) { return (int)max((int64_t)chunk_min, (v + 127) & ~(int64_t)127); };
   const int several = round_up((mean + 1) / 2);  // at most 2 slots + a unit per sequence and head
-  Chunking c{};
-  c.len = round_up(mean);
-  for (int64_t n = units(c.len); n > slots; n = units(c.len)) {
-    if (c.len > mean + several / 2 + 400) {
-      c.len = several;
-      break;
-    }
-    c.len = round_up(c.len + c.len / 16 + 1);
+  int len = round_up(mean);
+  if (units(1 << 30) > slots) return several;  // (no sequence is longer)
+  while (units(len) > slots) {
+    if (len > mean + several / 2 + 400) return several;
+    len = round_up(len + len / 16 + 1);
   }
-  int base = 0;
-  for (int b0 = 0; b0 < a.B; b0 += 64) {
-    if (a.B > 64) load(b0 + lane);
-    const int nc = chunks(c.len);
-    const int incl = wave_scan(nc);
-    const int first = base + incl - nc;
-    const uint64_t mine = __builtin_amdgcn_ballot_w64(nc > 0 && unit >= Hkv * first && unit < Hkv * (first + nc));
-    if (mine) {
-      const int o = __builtin_ctzll(mine);
-      c.found = true;
-      c.b = b0 + o;
-      c.nchunk = __builtin_amdgcn_readlane(nc, o);
-      c.unit0 = Hkv * __builtin_amdgcn_readlane(first, o);
-      c.head = uniform((unit - c.unit0) / c.nchunk);
-      c.chunk = unit - c.unit0 - c.head * c.nchunk;
-      c.s.q0 = __builtin_amdgcn_readlane(s.q0, o);
-      c.s.rows = __builtin_amdgcn_readlane(s.rows, o);
-      c.s.keys = __builtin_amdgcn_readlane(s.keys, o);
-      c.s.pos0 = __builtin_amdgcn_readlane(s.pos0, o);
-      return c;
-    }
-    base += __builtin_amdgcn_readlane(incl, 63);
-  }
-  return c;
+  return len;
 }
 
 // The rows of a chunk that the second kernel joins: per (sequence) where its units start.
 struct alignas(16) Joint {
   int q0, rows, nchunk, unit0;
 };
+
+// The plan of a call of more than 64 sequences, made by a kernel of its own: the sequences'
+// joints and first tiles, and what they come from.
+struct alignas(16) Plan {
+  int len, tiles, pad[2];
+};
+
+// The last of `n` ascending numbers that is not above x; the first is not.
+template <typename First>
+__device__ __forceinline__ int last_not_above(int n, int x, First first) {
+  const int lane = (int)__builtin_amdgcn_workitem_id_x() & 63;
+  int lo = 0;
+  while (n > 1) {
+    const int step = (n + 63) >> 6, i = lane * step;
+    const bool below = i < n && first(lo + min(i, n - 1)) <= x;
+    const int k = __builtin_popcountll(__builtin_amdgcn_ballot_w64(below)) - 1;
+    lo += k * step;
+    n = min(step, n - k * step);
+  }
+  return lo;
+}
+
+// What unit `unit` is.  Without a plan (up to 64 sequences, one a lane) every wave works it out for
+// itself.
+__device__ __forceinline__ Chunking find_chunk(const PagedAttentionArgs& a, int log2p, int Hkv,
+                                               int few_rows, int slots, int chunk_min,
+                                               const Plan* plan, const Joint* joints, int unit) {
+  const int lane = (int)__builtin_amdgcn_workitem_id_x() & 63;
+  const int G = a.Hq / Hkv;
+  Chunking c{};
+  if (plan) {
+    c.b = last_not_above(a.B, unit, [&](int b) { return joints[b].unit0; });
+    const Joint j = joints[c.b];
+    c.len = plan->len;
+    c.nchunk = uniform(j.nchunk);
+    c.unit0 = uniform(j.unit0);
+    c.found = unit - c.unit0 < Hkv * c.nchunk;
+    c.s = sequence(a, log2p, G, c.b);
+  } else {
+    Seq s{};
+    if (lane < a.B) s = sequence(a, log2p, G, lane);
+    if (s.rows > few_rows) s.rows = 0;
+    auto chunks = [&](int len) { return s.rows ? max(1, (s.keys + len - 1) / len) : 0; };
+    c.len = chunk_length(wave_add(s.rows ? (s.keys + 127) >> 7 : 0), Hkv, slots, chunk_min,
+                         [&](int len) { return Hkv * wave_add(chunks(len)); });
+    const int nc = chunks(c.len);
+    const int first = wave_scan(nc) - nc;
+    const uint64_t mine =
+        __builtin_amdgcn_ballot_w64(nc > 0 && unit >= Hkv * first && unit < Hkv * (first + nc));
+    if (!mine) return c;
+    c.found = true;
+    c.b = __builtin_ctzll(mine);
+    c.nchunk = __builtin_amdgcn_readlane(nc, c.b);
+    c.unit0 = Hkv * __builtin_amdgcn_readlane(first, c.b);
+    c.s.q0 = __builtin_amdgcn_readlane(s.q0, c.b);
+    c.s.rows = __builtin_amdgcn_readlane(s.rows, c.b);
+    c.s.keys = __builtin_amdgcn_readlane(s.keys, c.b);
+    c.s.pos0 = __builtin_amdgcn_readlane(s.pos0, c.b);
+  }
+  if (!c.found) return c;
+  c.head = uniform((unit - c.unit0) / c.nchunk);
+  c.chunk = unit - c.unit0 - c.head * c.nchunk;
+  return c;
+}
 
 template <int D>
 struct Block {
@@ -175,13 +191,13 @@ __device__ __forceinline__ void rotate_wave(float (&x)[D / 64], int lane) {
   for (int e = 0; e < D / 64; ++e) x[e] *= hadamard_norm<D>();
 }
 
-// A finished row: o / l (0 where nothing was seen), rotated back if asked, rounded once.  The
+// A finished row: o / l (0 where nothing was seen; NaN stays), rotated back if asked, rounded once.  The
 // wave holds channels lane * D / 64 and on.
 template <int D>
 __device__ __forceinline__ void store_row(const PagedAttentionArgs& a, int row, int hq, float (&o)[D / 64],
                                           float l, int lane) {
 #pragma unroll
-  for (int e = 0; e < D / 64; ++e) o[e] = l > 0.0f ? o[e] / l : 0.0f;
+  for (int e = 0; e < D / 64; ++e) o[e] = l == 0.0f ? 0.0f : o[e] / l;
   if (a.v_had) rotate_wave<D>(o, lane);
   uint16_t* dst = a.out + (int64_t)row * a.ldo + (int64_t)hq * D;
   if constexpr (D == 128) reinterpret_cast<uint32_t*>(dst)[lane] = bf16x2_rne(o[0], o[1]);
@@ -191,6 +207,7 @@ __device__ __forceinline__ void store_row(const PagedAttentionArgs& a, int row, 
 template <int D, int RT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void
 kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, int slots,
+                              int chunk_min, const Plan* __restrict__ plan,
                               Joint* __restrict__ joints, float* __restrict__ rec) {
   constexpr int NW = D / 32;  // key code words of a lane
   constexpr int NM = D / 16;  // products of a value block: 16 columns of NM channels each
@@ -209,11 +226,10 @@ kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, 
   const int pr = lane & 15, kq = lane >> 4;
   const int unit = (int)__builtin_amdgcn_workgroup_id_x();
   const int G = a.Hq / c.Hkv;
-  const Chunking w = find_chunk(a, c.log2p, c.Hkv, few_rows, slots,
-                                joints ? CHUNK_MIN : CHUNK_ONE, unit);
+  const Chunking w = find_chunk(a, c.log2p, c.Hkv, few_rows, slots, chunk_min, plan, joints, unit);
   if (!w.found) return;
   const int rows = w.s.rows, hk = w.head;
-  if (joints && w.chunk == 0 && hk == 0 && tid == 0)
+  if (joints && !plan && w.chunk == 0 && hk == 0 && tid == 0)
     joints[w.b] = Joint{w.s.q0, rows, w.nchunk, w.unit0};
   // the wave's positions: a quarter of the chunk
   const int k_end = min(w.s.keys, (w.chunk + 1) * w.len);
@@ -687,42 +703,94 @@ struct Tile {
   Seq s;
 };
 // Tile number `t` of all sequences' tiles, counted from the last: the longest of a sequence first.
+// Without a plan (up to 64 sequences, one a lane) every wave works it out for itself.  `tiles`: what
+// there is room for, all of them where the starts ascend.
+__device__ __forceinline__ int tiles_of(const Seq& s, int few_rows) {
+  return s.rows > few_rows ? (s.rows + ROWS - 1) / ROWS : 0;
+}
 __device__ __forceinline__ Tile find_tile(const PagedAttentionArgs& a, int log2p, int G, int few_rows,
-                                          int t) {
+                                          int tiles, const Plan* plan, const int* starts, int t) {
   const int lane = (int)__builtin_amdgcn_workitem_id_x() & 63;
-  Seq s{};
-  auto load = [&](int b) {
-    s = Seq{};
-    if (b < a.B) s = sequence(a, log2p, G, b);
-    return s.rows > few_rows ? (s.rows + ROWS - 1) / ROWS : 0;
-  };
-  int count = 0, mine = 0;
-  for (int b0 = 0; b0 < a.B; b0 += 64) count += mine = load(b0 + lane);
-  count = wave_add(count);
   Tile r{};
-  r.count = count;
-  if (t >= count) return r;
-  r.index = count - 1 - t;
-  int base = 0;
-  for (int b0 = 0; b0 < a.B; b0 += 64) {
-    if (a.B > 64) mine = load(b0 + lane);
-    const int incl = wave_scan(mine);
-    const int first = base + incl - mine;
-    const uint64_t hit = __builtin_amdgcn_ballot_w64(r.index >= first && r.index < first + mine);
-    if (hit) {
-      const int o = __builtin_ctzll(hit);
-      r.found = true;
-      r.b = b0 + o;
-      r.i = r.index - __builtin_amdgcn_readlane(first, o);
-      r.s.q0 = __builtin_amdgcn_readlane(s.q0, o);
-      r.s.rows = __builtin_amdgcn_readlane(s.rows, o);
-      r.s.keys = __builtin_amdgcn_readlane(s.keys, o);
-      r.s.pos0 = __builtin_amdgcn_readlane(s.pos0, o);
-      return r;
-    }
-    base += __builtin_amdgcn_readlane(incl, 63);
+  if (plan) {
+    r.count = min(plan->tiles, tiles);
+    r.found = t < r.count;
+    if (!r.found) return r;
+    r.index = r.count - 1 - t;
+    r.b = last_not_above(a.B, r.index, [&](int b) { return starts[b]; });
+    r.i = r.index - uniform(starts[r.b]);
+    r.s = sequence(a, log2p, G, r.b);
+    return r;
   }
+  Seq s{};
+  if (lane < a.B) s = sequence(a, log2p, G, lane);
+  const int mine = tiles_of(s, few_rows);
+  const int incl = wave_scan(mine);
+  r.count = min(__builtin_amdgcn_readlane(incl, 63), tiles);
+  r.found = t < r.count;
+  if (!r.found) return r;
+  r.index = r.count - 1 - t;
+  const uint64_t hit =
+      __builtin_amdgcn_ballot_w64(r.index >= incl - mine && r.index < incl);
+  r.b = __builtin_ctzll(hit);
+  r.i = r.index - __builtin_amdgcn_readlane(incl - mine, r.b);
+  r.s.q0 = __builtin_amdgcn_readlane(s.q0, r.b);
+  r.s.rows = __builtin_amdgcn_readlane(s.rows, r.b);
+  r.s.keys = __builtin_amdgcn_readlane(s.keys, r.b);
+  r.s.pos0 = __builtin_amdgcn_readlane(s.pos0, r.b);
   return r;
+}
+
+// The plan of a call of more than 64 sequences, by one workgroup.  (Worked out by every wave, 64
+// sequences at a time, one token after 512 x 500 positions took 361 us, after 1024 x 300 722.)
+__global__ __launch_bounds__(1024) void kv_attention_paged_plan_kernel(
+    PagedAttentionArgs a, int log2p, int Hkv, int few_rows, int slots, int chunk_min,
+    Plan* __restrict__ plan, Joint* __restrict__ joints, int* __restrict__ starts) {
+  __shared__ int64_t s_sum[16];
+  __shared__ int2 s_scan[16];
+  const int tid = (int)__builtin_amdgcn_workitem_id_x();
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int G = a.Hq / Hkv;
+  auto at = [&](int b) {
+    Seq s{};
+    if (b < a.B) s = sequence(a, log2p, G, b);
+    return s;
+  };
+  auto few = [&](const Seq& s) { return s.rows > 0 && s.rows <= few_rows; };
+  auto chunks = [&](const Seq& s, int len) { return few(s) ? max(1, (s.keys + len - 1) / len) : 0; };
+  auto total = [&](auto value) {  // over all sequences
+    int64_t sum = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 1024) sum += wave_add(value(at(b0 + tid)));
+    __syncthreads();
+    if (lane == 0) s_sum[wave] = sum;
+    __syncthreads();
+    sum = 0;
+    for (int k = 0; k < 16; ++k) sum += s_sum[k];
+    return sum;
+  };
+  const int64_t blocks = total([&](const Seq& s) { return few(s) ? (s.keys + 127) >> 7 : 0; });
+  const int len = chunk_length(blocks, Hkv, slots, chunk_min, [&](int len) {
+    return Hkv * total([&](const Seq& s) { return chunks(s, len); });
+  });
+  int2 base = make_int2(0, 0);  // units of a head, tiles
+  for (int b0 = 0; b0 < a.B; b0 += 1024) {
+    const Seq s = at(b0 + tid);
+    const int nc = chunks(s, len), nt = tiles_of(s, few_rows);
+    const int2 incl = make_int2(wave_scan(nc), wave_scan(nt));
+    __syncthreads();
+    if (lane == 63) s_scan[wave] = incl;
+    __syncthreads();
+    int2 before = base;
+    for (int k = 0; k < 16; ++k) {
+      if (k < wave) before = make_int2(before.x + s_scan[k].x, before.y + s_scan[k].y);
+      base = make_int2(base.x + s_scan[k].x, base.y + s_scan[k].y);
+    }
+    if (b0 + tid < a.B) {
+      joints[b0 + tid] = Joint{s.q0, few(s) ? s.rows : 0, nc, Hkv * (before.x + incl.x - nc)};
+      starts[b0 + tid] = before.y + incl.y - nt;
+    }
+  }
+  if (tid == 0) *plan = Plan{len, base.y, {0, 0}};
 }
 
 // The rows of a tile that the second kernel joins.
@@ -732,8 +800,8 @@ struct alignas(16) TileJoint {
 
 template <int D>
 __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
-    PagedAttentionArgs a, PagedCache c, int few_rows, int tiles, int splits, TileJoint* __restrict__ joints,
-    float* __restrict__ rec) {
+    PagedAttentionArgs a, PagedCache c, int few_rows, int tiles, int splits, const Plan* __restrict__ plan,
+    const int* __restrict__ starts, TileJoint* __restrict__ joints, float* __restrict__ rec) {
   constexpr int KROW = 2 * D + 16;
   constexpr int NS = D / 16;   // k-steps of the score product
   constexpr int ND = D / 32;   // tiles of output channels
@@ -750,7 +818,7 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
   // whole XCDs idle)
   const int hk = uniform(id % c.Hkv), t = uniform(id / c.Hkv % tiles);
   const int split = uniform(id / c.Hkv / tiles);
-  const Tile w = find_tile(a, c.log2p, G, few_rows, t);
+  const Tile w = find_tile(a, c.log2p, G, few_rows, tiles, plan, starts, t);
   if (!w.found) {
     if (joints && !split && !hk && !tid) joints[t] = TileJoint{0, 0, 0, 0};
     return;
@@ -923,6 +991,7 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
   // code words; without a rotation the product is with 1.
   uint32_t qb[NS][4], zb[4] = {0, 0, 0, 0};
   int E;
+  bool bad;  // the row is not finite: held at the end of fp16's range, it would give numbers
   {
     const int ch = 16 * ((ql >> 2) & 1) + 4 * (ql >> 3) + (ql & 3);
     auto entry = [&](int k) {
@@ -968,25 +1037,40 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
           }
       sm2 *= hadamard_norm<D>();
     }
-    // E: the largest query at 2^4 at most (a block whose keys would leave their range raises it)
+    // E: the largest query at 2^4, unless the first block's keys would leave their range.  Then
+    // queries beyond fp16's range stay at its end: scores over 2^25, where the others, in the same
+    // tile, keep their bits.
     float qm = 0.0f;
 #pragma unroll
     for (int i = 0; i < D / 2; ++i) qm = fmaxf(qm, fabsf(x[i >> 4][i & 15]));
     qm = wave_max(qm);
+    const float kt = wave_max(any && (uint32_t)fpage[0] < (uint32_t)c.pages &&
+                                      kb0 * KB + lane < keys
+                                  ? fp16_bits_to_f32((uint16_t)fpar[0].x) *
+                                        (8192.0f + fabsf((float)(int16_t)(fpar[0].x >> 16)))
+                                  : 0.0f);
     if (lane == 0) s_qm[wave] = qm;
     __syncthreads();
     qm = s_qm[0];
 #pragma unroll
     for (int k = 1; k < 8; ++k) qm = fmaxf(qm, s_qm[k]);
     E = uniform(-5 - max(__builtin_amdgcn_frexp_expf(qm), -100) - __builtin_amdgcn_frexp_expf(sm2));
+    if (kt > 0.0f) E = max(E, uniform(__builtin_amdgcn_frexp_expf(kt)) - 25);
     const float f = __builtin_amdgcn_ldexpf(sm2, E + 9);
+    float check = 0.0f;
+#pragma unroll
+    for (int i = 0; i < D / 2; ++i) check = __builtin_fmaf(x[i >> 4][i & 15], 0.0f, check);
+    check += __shfl_xor(check, 32);
+    bad = check != 0.0f;
     float sum = 0.0f;
 #pragma unroll
     for (int s = 0; s < NS; ++s)
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const h2_t p = {(_Float16)(f * x[s >> 1][8 * (s & 1) + k]),
-                        (_Float16)(f * x[s >> 1][8 * (s & 1) + k + 4])};
+        const h2_t top = {(_Float16)65504.0f, (_Float16)65504.0f};
+        h2_t p = {(_Float16)(f * x[s >> 1][8 * (s & 1) + k]),
+                  (_Float16)(f * x[s >> 1][8 * (s & 1) + k + 4])};
+        p = __builtin_elementwise_max(__builtin_elementwise_min(p, top), -top);
         sum = __builtin_amdgcn_fdot2(p, h2_t{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
         qb[s][k] = __builtin_bit_cast(uint32_t, p);
       }
@@ -1168,6 +1252,7 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
   }
   if (wrow > last) return;
   l += __shfl_xor(l, 32);
+  if (bad && l > 0.0f) l = __builtin_nanf("");
 
   // ---- channels: o[d][r] is channel 8 word + nibble of V^T's row 32 d + 8 (r / 4) + 4 h + r % 4
   // = nibble * D / 8 + word
@@ -1182,7 +1267,7 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
     if (!mine) return;
     float* dst = rec + (int64_t)((w.index * c.Hkv + hk) * splits + split) * ROWS * (D + 2);
     const int i = 32 * wave + ql;
-    if (!h) *reinterpret_cast<float2*>(dst + 2 * i) = make_float2(l > 0.0f ? -neg[0] : LOWEST, l);
+    if (!h) *reinterpret_cast<float2*>(dst + 2 * i) = make_float2(l == 0.0f ? LOWEST : -neg[0], l);
     dst += 2 * ROWS + i * D;
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) {
@@ -1194,7 +1279,7 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
     }
     return;
   }
-  const float f = l > 0.0f ? back / l : 0.0f;
+  const float f = l == 0.0f ? 0.0f : back / l;
 #pragma unroll
   for (int d = 0; d < ND; ++d) o[d] *= f;
   if (a.v_had) {  // every channel bit is a bit of d, r or h
@@ -1259,7 +1344,7 @@ namespace {
 // How a call is launched: the rows that the few-row kernel takes, its row tiles and units; the
 // tiles of the other kernel and over how many workgroups the keys of each are split.
 struct Shape {
-  bool few, many, few_join;
+  bool few, many, few_join, plan;
   int few_rows, row_tiles, slots, units;
   int64_t tiles;
   int splits;
@@ -1279,6 +1364,7 @@ Shape attention_shape(int64_t M, int64_t B, int64_t Hq, int64_t Hkv, int D, int6
   f.few_rows = f.few ? (int)(f.many ? 16 : most) : 0;
   f.slots = 512;  // two workgroups a CU
   f.few_join = f.few && cap > CHUNK_ONE;
+  f.plan = B > 64;
   f.units = (int)((f.few_join ? 2 * f.slots : 0) + B * Hkv);
   f.splits = 1;
   if (f.many) {
@@ -1294,8 +1380,12 @@ Shape attention_shape(int64_t M, int64_t B, int64_t Hq, int64_t Hkv, int D, int6
   }
   return f;
 }
+// The workspace: the plan and the sequences' first tiles where there is one, the sequences' joints,
+// the chunks' rows; then the tiles' joints and rows.
+int64_t plan_floats(const Shape& f, int64_t B) { return f.plan ? 4 + (B + 3) / 4 * 4 : 0; }
 int64_t few_floats(const Shape& f, int64_t B, int D) {
-  return f.few_join ? 4 * B + (int64_t)f.units * f.few_rows * (D + 2) : 0;
+  const int64_t joints = f.plan || f.few_join ? 4 * B : 0;
+  return joints + (f.few_join ? ((int64_t)f.units * f.few_rows * (D + 2) + 3) / 4 * 4 : 0);
 }
 int64_t tile_floats(const Shape& f, int64_t Hkv, int D) {
   return f.splits > 1 ? 4 * f.tiles + f.tiles * Hkv * f.splits * ROWS * (D + 2) : 0;
@@ -1306,18 +1396,25 @@ int64_t tile_floats(const Shape& f, int64_t Hkv, int D) {
 int64_t kv_attention_paged_workspace_floats(int64_t M, int64_t B, int64_t Hq, int64_t Hkv,
                                             int head_dim, int64_t max_new) {
   const Shape f = attention_shape(M, B, Hq, Hkv, head_dim, max_new, int64_t(1) << 30);
-  return (few_floats(f, B, head_dim) + 3) / 4 * 4 + tile_floats(f, Hkv, head_dim);
+  return plan_floats(f, B) + few_floats(f, B, head_dim) + tile_floats(f, Hkv, head_dim);
 }
 
 hipError_t launch_kv_attention_paged(const PagedAttentionArgs& a, const PagedCache& c, int head_dim,
                                      float* workspace, hipStream_t stream) {
   const Shape f = attention_shape(a.M, a.B, a.Hq, c.Hkv, head_dim, a.max_new, (int64_t)a.max_pages << c.log2p);
+  Plan* plan = f.plan ? reinterpret_cast<Plan*>(workspace) : nullptr;
+  int* starts = reinterpret_cast<int*>(workspace) + 4;
+  float* few_at = workspace + plan_floats(f, a.B);
+  Joint* joints = f.plan || f.few_join ? reinterpret_cast<Joint*>(few_at) : nullptr;
+  const int chunk_min = f.few_join ? CHUNK_MIN : CHUNK_ONE;
+  if (plan)
+    hipLaunchKernelGGL(kv_attention_paged_plan_kernel, dim3(1), dim3(1024), 0, stream, a, c.log2p, c.Hkv,
+                       f.few_rows, f.slots, chunk_min, plan, joints, starts);
   if (f.few) {
-    Joint* joints = f.few_join ? reinterpret_cast<Joint*>(workspace) : nullptr;
-    float* rec = workspace + 4 * (int64_t)a.B;
+    float* rec = few_at + 4 * (int64_t)a.B;
 #define OFFQ_FEW(D_, RT_)                                                                        \
   hipLaunchKernelGGL((kv_attention_paged_few_kernel<D_, RT_>), dim3((unsigned)f.units), dim3(256), \
-                     0, stream, a, c, f.few_rows, f.slots, joints, rec)
+                     0, stream, a, c, f.few_rows, f.slots, chunk_min, plan, joints, rec)
     if (head_dim == 128) {
       if (f.row_tiles == 1) OFFQ_FEW(128, 1);
       else if (f.row_tiles == 2) OFFQ_FEW(128, 2);
@@ -1336,13 +1433,13 @@ hipError_t launch_kv_attention_paged(const PagedAttentionArgs& a, const PagedCac
                          f.few_rows, joints, rec, c.log2p, f.few_rows);
   }
   if (f.many) {
-    float* base = workspace + (few_floats(f, a.B, head_dim) + 3) / 4 * 4;
+    float* base = few_at + few_floats(f, a.B, head_dim);
     TileJoint* joints = f.splits > 1 ? reinterpret_cast<TileJoint*>(base) : nullptr;
     float* rec = base + 4 * f.tiles;
     const dim3 grid((unsigned)(f.tiles * c.Hkv * f.splits));
     hipLaunchKernelGGL(head_dim == 128 ? kv_attention_paged_tile_kernel<128>
                                        : kv_attention_paged_tile_kernel<64>,
-                       grid, dim3(512), 0, stream, a, c, f.few_rows, (int)f.tiles, f.splits, joints, rec);
+                       grid, dim3(512), 0, stream, a, c, f.few_rows, (int)f.tiles, f.splits, plan, starts, joints, rec);
     if (f.splits > 1)
       hipLaunchKernelGGL(head_dim == 128 ? kv_attention_paged_tile_join_kernel<128>
                                          : kv_attention_paged_tile_join_kernel<64>,

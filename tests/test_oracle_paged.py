@@ -211,3 +211,17 @@ def test_workspace_bytes():
         for short in (dict(workspace_bytes=need - 1), dict(workspace=None)):
             assert _lib.offq_kv_attention_paged_raw(*{**ATTEND, **short}.values()) == BAD
             assert "workspace" in _lib.last_error()
+
+
+def test_more_threads_than_a_launch_has():
+    """A wave per token, head_dim / 8 lanes per row, a workgroup per joined row: under 2^32 threads."""
+    assert _lib.offq_rope_kv_paged_raw(*{**WRITE, "M": (1 << 26) - 3, "q_out": 1 << 45}.values()) == UNS
+    for change in (dict(M=1 << 28, Hkv=2, head_dim=64), dict(M=1 << 24, Hkv=16, head_dim=128)):
+        D = change["head_dim"] * change["Hkv"]
+        big = {**READ, **change, "k_out": 1 << 44, "v_out": 1 << 46, "ldk": D, "ldv": D}
+        assert _lib.offq_kv_dequantize_paged_raw(*big.values()) == UNS
+    f = _lib.offq_kv_attention_paged_workspace_bytes
+    many = dict(B=1 << 17, Hkv=2)
+    assert f(1 << 17, many["B"], 4, many["Hkv"], 128, 1) == 0
+    assert _lib.offq_kv_attention_paged_raw(*{**ATTEND, **many}.values()) == UNS
+    assert f(1 << 16, 1 << 16, 4, 2, 128, 1) > 0
