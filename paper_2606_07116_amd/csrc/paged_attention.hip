@@ -1210,9 +1210,32 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
       const int4 x = *reinterpret_cast<const int4*>(&S.par[kb & 3].E);
       return make_int4(uniform(x.x), uniform(x.y), uniform(x.z), uniform(x.w));
     };
+    auto stage_keys = [&](int kb, int slot) {
+      store_k(kb + 2, slot);
+      load_k(min(kb + 3, kbl));
+    };
+    auto stage_values = [&](int kb, int slot) {
+      store_v(kb + 1, slot);
+      load_v(min(kb + 2, kbl));
+      if (((kb - kb0) & 7) == wave) {
+        const int4 before = meta(kb + 2);
+        prepare(kb + 3, page0, par0, before.x, before.y);
+        page0 = page1;
+        par0 = params(kb + 11, page0);
+        page1 = page_of(kb + 19);
+      }
+    };
     int4 now = meta(kb0);
     rescale_q(now.x);
     lds_barrier();
+    if (wrow > last) {  // no rows: only the staging, in step with the others
+      for (int kb = kb0, s2 = 2, v1 = 1; kb < kb1; ++kb, s2 = s2 == 2 ? 0 : s2 + 1, v1 ^= 1) {
+        stage_keys(kb, s2);
+        stage_values(kb, v1);
+        lds_barrier();
+      }
+      return;
+    }
     f16_t s0, s1;
     scores(kb0, 0, 0, s0);
     int sl = 0, vs = 0;  // slots of this block's keys and values
@@ -1230,23 +1253,14 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
       float sum = weights(s0, l);
       settle(s0, s1, sum);
       values(vs, 0);
-      store_k(kb + 2, sl2);
-      load_k(min(kb + 3, kbl));
+      stage_keys(kb, sl2);
       mask(s1, kb * KB + 32, (uint32_t)now.w);
       rescale_q(next.x);
       scores(kb + 1, sl1, 0, s0);
       sum = weights(s1, l);
       settle(s1, s0, sum);
       values(vs, 1);
-      store_v(kb + 1, vs ^ 1);
-      load_v(min(kb + 2, kbl));
-      if (((kb - kb0) & 7) == wave) {
-        const int4 before = meta(kb + 2);
-        prepare(kb + 3, page0, par0, before.x, before.y);
-        page0 = page1;
-        par0 = params(kb + 11, page0);
-        page1 = page_of(kb + 19);
-      }
+      stage_values(kb, vs ^ 1);
       lds_barrier();
       now = next;
       sl = sl1;
