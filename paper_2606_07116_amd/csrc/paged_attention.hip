@@ -1393,7 +1393,8 @@ Shape attention_shape(int64_t M, int64_t B, int64_t Hq, int64_t Hkv, int D, int6
     f.tiles = (M * G + (ROWS - 1) * (B < M ? B : M)) / ROWS;
     const int64_t wgs = f.tiles * Hkv;
     // one workgroup per CU: the fewest splits that keep nine in ten of 256 CUs busy
-    for (int s = 1; s <= 64 && wgs * s <= 768; ++s) {
+    const int64_t most_splits = cap / (4 * KB);  // (that the kernel makes)
+    for (int s = 1; s <= 64 && wgs * s <= 768 && (s == 1 || s <= most_splits); ++s) {
       f.splits = s;
       const int64_t rounds = (wgs * s + 255) / 256;
       if (10 * wgs * s >= 9 * 256 * rounds) break;
