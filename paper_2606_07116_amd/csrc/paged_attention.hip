@@ -565,64 +565,6 @@ kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, 
   }
 }
 
-// Joins the chunks of a row: one workgroup per (sequence, key/value head, row), four waves over
-// the chunks.
-template <int D>
-__global__ __launch_bounds__(256) void kv_attention_paged_join_kernel(
-    PagedAttentionArgs a, int Hkv, int cap, const Joint* __restrict__ joints,
-    const float* __restrict__ rec, int log2p, int few_rows) {
-  __shared__ float s_o[4][D], s_ml[2][4];
-  const int lane = (int)__builtin_amdgcn_workitem_id_x() & 63;
-  const int wave = __builtin_amdgcn_readfirstlane((int)__builtin_amdgcn_workitem_id_x() >> 6);
-  const int G = a.Hq / Hkv;
-  const int id = (int)__builtin_amdgcn_workgroup_id_x();
-  const int hk = id % Hkv, row = id / Hkv % cap, b = id / Hkv / cap;
-  const Seq s = sequence(a, log2p, G, b);
-  if (row >= s.rows || s.rows > few_rows) return;
-  const Joint j = joints[b];
-  if (j.nchunk <= 1) return;
-  const int64_t size = (int64_t)cap * (D + 2);
-  const float* first = rec + (int64_t)(j.unit0 + hk * j.nchunk) * size;
-  float top = LOWEST;
-  for (int i = lane; i < j.nchunk; i += 64) top = fmaxf(top, first[i * size + 2 * row]);
-  top = wave_max(top);
-  float l = 0.0f, o[D / 64] = {};
-  for (int i0 = 64 * wave; i0 < j.nchunk; i0 += 256) {
-    float f = 0.0f;
-    if (i0 + lane < j.nchunk) {
-      const float2 ml = *reinterpret_cast<const float2*>(first + (i0 + lane) * size + 2 * row);
-      f = __builtin_amdgcn_exp2f(ml.x - top);
-      l = __builtin_fmaf(f, ml.y, l);
-    }
-    const int n = min(64, j.nchunk - i0);
-    const float* src = first + i0 * size + 2 * cap + row * D + lane * (D / 64);
-    for (int k = 0; k < n; k += 8) {  // (factors past the last chunk are 0)
-      float v[8][D / 64];
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int e = 0; e < D / 64; ++e) v[i][e] = src[min(k + i, n - 1) * size + e];
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int e = 0; e < D / 64; ++e) o[e] = __builtin_fmaf(__shfl(f, k + i), v[i][e], o[e]);
-    }
-  }
-  l = wave_sum(l);
-  if (lane == 0) s_ml[0][wave] = l;
-#pragma unroll
-  for (int e = 0; e < D / 64; ++e) s_o[wave][lane * (D / 64) + e] = o[e];
-  __syncthreads();
-  if (wave) return;
-#pragma unroll
-  for (int e = 0; e < D / 64; ++e) {
-    const int d = lane * (D / 64) + e;
-    o[e] = (s_o[0][d] + s_o[1][d]) + (s_o[2][d] + s_o[3][d]);
-  }
-  l = (s_ml[0][0] + s_ml[0][1]) + (s_ml[0][2] + s_ml[0][3]);
-  store_row<D>(a, j.q0 + row / G, hk * G + row % G, o, l, lane);
-}
-
 // ---------------------------------------------------------------------------
 // Many rows: tiles of 256 query rows (new tokens x heads of a group) of a sequence and
 // key/value head, eight waves of 32 rows, over blocks of 64 positions.  With many queries per
@@ -1325,19 +1267,84 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
   }
 }
 
-// Joins the splits of a tile's rows, a wave per row.
+// What a call's chunks or splits left: who they belong to, and their rows.
+struct FewJoin {
+  const Joint* joints;
+  const float* rec;
+  int rows, blocks;  // the most rows of a sequence and head; workgroups
+};
+struct TileJoin {
+  const TileJoint* joints;
+  const float* rec;
+  int splits, blocks;
+};
+
+// Joins the chunks of a row: one workgroup per (sequence, key/value head, row), four waves over
+// the chunks.
 template <int D>
-__global__ __launch_bounds__(256) void kv_attention_paged_tile_join_kernel(
-    PagedAttentionArgs a, int Hkv, int splits, const TileJoint* __restrict__ joints,
-    const float* __restrict__ rec) {
+__device__ __forceinline__ void join_chunks(const PagedAttentionArgs& a, int Hkv, int log2p,
+                                            const FewJoin& w, int id) {
+  __shared__ float s_o[4][D], s_ml[2][4];
   const int lane = (int)__builtin_amdgcn_workitem_id_x() & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)__builtin_amdgcn_workitem_id_x() >> 6);
-  const int id = (int)__builtin_amdgcn_workgroup_id_x();
+  const int G = a.Hq / Hkv;
+  const int hk = id % Hkv, row = id / Hkv % w.rows, b = id / Hkv / w.rows;
+  const Seq s = sequence(a, log2p, G, b);
+  if (row >= s.rows || s.rows > w.rows) return;
+  const Joint j = w.joints[b];
+  if (j.nchunk <= 1) return;
+  const int64_t size = (int64_t)w.rows * (D + 2);
+  const float* first = w.rec + (int64_t)(j.unit0 + hk * j.nchunk) * size;
+  float top = LOWEST;
+  for (int i = lane; i < j.nchunk; i += 64) top = fmaxf(top, first[i * size + 2 * row]);
+  top = wave_max(top);
+  float l = 0.0f, o[D / 64] = {};
+  for (int i0 = 64 * wave; i0 < j.nchunk; i0 += 256) {
+    float f = 0.0f;
+    if (i0 + lane < j.nchunk) {
+      const float2 ml = *reinterpret_cast<const float2*>(first + (i0 + lane) * size + 2 * row);
+      f = __builtin_amdgcn_exp2f(ml.x - top);
+      l = __builtin_fmaf(f, ml.y, l);
+    }
+    const int n = min(64, j.nchunk - i0);
+    const float* src = first + i0 * size + 2 * w.rows + row * D + lane * (D / 64);
+    for (int k = 0; k < n; k += 8) {  // (factors past the last chunk are 0)
+      float v[8][D / 64];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int e = 0; e < D / 64; ++e) v[i][e] = src[min(k + i, n - 1) * size + e];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int e = 0; e < D / 64; ++e) o[e] = __builtin_fmaf(__shfl(f, k + i), v[i][e], o[e]);
+    }
+  }
+  l = wave_sum(l);
+  if (lane == 0) s_ml[0][wave] = l;
+#pragma unroll
+  for (int e = 0; e < D / 64; ++e) s_o[wave][lane * (D / 64) + e] = o[e];
+  __syncthreads();
+  if (wave) return;
+#pragma unroll
+  for (int e = 0; e < D / 64; ++e) {
+    const int d = lane * (D / 64) + e;
+    o[e] = (s_o[0][d] + s_o[1][d]) + (s_o[2][d] + s_o[3][d]);
+  }
+  l = (s_ml[0][0] + s_ml[0][1]) + (s_ml[0][2] + s_ml[0][3]);
+  store_row<D>(a, j.q0 + row / G, hk * G + row % G, o, l, lane);
+}
+
+// Joins the splits of a tile's rows, a wave per row.
+template <int D>
+__device__ __forceinline__ void join_splits(const PagedAttentionArgs& a, int Hkv, const TileJoin& w, int id) {
+  const int lane = (int)__builtin_amdgcn_workitem_id_x() & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((int)__builtin_amdgcn_workitem_id_x() >> 6);
   const int i = 4 * (id % (ROWS / 4)) + wave, hk = id / (ROWS / 4) % Hkv, t = id / (ROWS / 4) / Hkv;
-  const TileJoint j = joints[t];
+  const TileJoint j = w.joints[t];
   if (i >= j.rows || j.nsplit <= 1) return;
   const int64_t size = ROWS * (D + 2);
-  const float* src = rec + (int64_t)(t * Hkv + hk) * splits * size;
+  const float* src = w.rec + (int64_t)(t * Hkv + hk) * w.splits * size;
   float2 ml = make_float2(LOWEST, 0.0f);  // splits <= 64
   if (lane < j.nsplit) ml = *reinterpret_cast<const float2*>(src + lane * size + 2 * i);
   const float top = wave_max(ml.x);
@@ -1352,6 +1359,15 @@ __global__ __launch_bounds__(256) void kv_attention_paged_tile_join_kernel(
   }
   const int G = a.Hq / Hkv, row = j.row0 + i;
   store_row<D>(a, j.q0 + row / G, hk * G + row % G, o, l, lane);
+}
+
+// (one launch for both: 1.5 us less where a call has both)
+template <int D>
+__global__ __launch_bounds__(256) void kv_attention_paged_join_kernel(PagedAttentionArgs a, int Hkv,
+                                                                      int log2p, FewJoin few, TileJoin tile) {
+  const int id = (int)__builtin_amdgcn_workgroup_id_x();
+  if (id < few.blocks) join_chunks<D>(a, Hkv, log2p, few, id);
+  else join_splits<D>(a, Hkv, tile, id - few.blocks);
 }
 
 }  // namespace
@@ -1432,6 +1448,8 @@ hipError_t launch_kv_attention_paged(const PagedAttentionArgs& a, const PagedCac
   if (plan)
     hipLaunchKernelGGL(kv_attention_paged_plan_kernel, dim3(1), dim3(1024), 0, stream, a, c.log2p, c.Hkv,
                        f.few_rows, 256 * f.per_cu, chunk_min, plan, joints, starts);
+  FewJoin few = {};
+  TileJoin tile = {};
   if (f.few) {
     float* rec = few_at + 4 * (int64_t)a.B;
 #define OFFQ_FEW(D_, RT_, W_)                                                                         \
@@ -1449,11 +1467,7 @@ hipError_t launch_kv_attention_paged(const PagedAttentionArgs& a, const PagedCac
       else OFFQ_FEW(64, 4, 2);
     }
 #undef OFFQ_FEW
-    if (f.few_join)
-      hipLaunchKernelGGL(head_dim == 128 ? kv_attention_paged_join_kernel<128>
-                                         : kv_attention_paged_join_kernel<64>,
-                         dim3((unsigned)(f.few_rows * c.Hkv * a.B)), dim3(256), 0, stream, a, c.Hkv,
-                         f.few_rows, joints, rec, c.log2p, f.few_rows);
+    if (f.few_join) few = FewJoin{joints, rec, f.few_rows, f.few_rows * c.Hkv * a.B};
   }
   if (f.many) {
     float* base = few_at + few_floats(f, a.B, head_dim);
@@ -1463,12 +1477,12 @@ hipError_t launch_kv_attention_paged(const PagedAttentionArgs& a, const PagedCac
     hipLaunchKernelGGL(head_dim == 128 ? kv_attention_paged_tile_kernel<128>
                                        : kv_attention_paged_tile_kernel<64>,
                        grid, dim3(512), 0, stream, a, c, f.few_rows, (int)f.tiles, f.splits, plan, starts, joints, rec);
-    if (f.splits > 1)
-      hipLaunchKernelGGL(head_dim == 128 ? kv_attention_paged_tile_join_kernel<128>
-                                         : kv_attention_paged_tile_join_kernel<64>,
-                         dim3((unsigned)(f.tiles * c.Hkv * (ROWS / 4))), dim3(256), 0, stream, a, c.Hkv,
-                         f.splits, joints, rec);
+    if (f.splits > 1) tile = TileJoin{joints, rec, f.splits, (int)(f.tiles * c.Hkv * (ROWS / 4))};
   }
+  if (few.blocks + tile.blocks)
+    hipLaunchKernelGGL(head_dim == 128 ? kv_attention_paged_join_kernel<128> : kv_attention_paged_join_kernel<64>,
+                       dim3((unsigned)(few.blocks + tile.blocks)), dim3(256), 0, stream, a, c.Hkv, c.log2p,
+                       few, tile);
   return hipGetLastError();
 }
 
