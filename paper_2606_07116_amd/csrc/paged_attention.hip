@@ -70,9 +70,9 @@ __device__ __forceinline__ Seq sequence(const PagedAttentionArgs& a, int log2p, 
 //
 // Measured (a large copy here: 4.9 TB/s, reads alone 6.2): 8 x 32768 positions of 32 heads of their
 // own 205 us, 5.5 TB/s; 24 ragged sequences of up to 30000, five query heads to each of 8, 75 us
-// with the join's 5; 16 x 4097 22 us for 71 MB.  A workgroup costs 8 us besides its positions'
+// with the join's 5; 16 x 4097 22 us for 71 MB.  A workgroup costs 6 us besides its positions'
 // bytes (who it is, page ids, first block, queries, the waves' join), which is what is left there
-// and below: one token after 300 positions 4.6 us.
+// and below: one token after 300 positions 8.4 us.
 struct Chunking {
   int len;          // positions per chunk, a multiple of 128
   int b, head, chunk, nchunk, unit0;  // this unit's; unit0: the sequence's first unit
