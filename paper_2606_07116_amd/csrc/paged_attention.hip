@@ -293,40 +293,51 @@ kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, 
   const bool any = k_begin < k_stop;
   if (any) load_block(k_begin, blk[0]);
 
-  // ---- queries: rotated, scaled by a power of two into the fp16 range, in operand order.  (A
-  // loop that stays one: unrolled, the code of the sixteen or more rows costs more to fetch than
-  // its work.)
+  // ---- queries: rotated, scaled by a power of two into the fp16 range, in operand order.  D / 8
+  // lanes a row.  (A loop that stays one: unrolled, its code costs more to fetch than its work.)
+  constexpr int LPH = D / 8, NG = 64 / LPH;
+  const int l8 = lane & (LPH - 1), g8 = lane / LPH;
   {
-    uint32_t next = 0;
+    uint4 next;
     auto fetch = [&](int r) {
-      const uint16_t* src = a.q + (int64_t)(w.s.q0 + r / G) * a.ldq + (int64_t)(hk * G + r % G) * D;
-      if constexpr (D == 128) next = reinterpret_cast<const uint32_t*>(src)[lane];
-      else next = src[lane];
+      r = min(r, rows - 1);
+      next = *reinterpret_cast<const uint4*>(a.q + (int64_t)(w.s.q0 + r / G) * a.ldq +
+                                             (int64_t)(hk * G + r % G) * D + 8 * l8);
     };
-    if (wave < rows) fetch(wave);
+    if (NG * wave < rows) fetch(NG * wave + g8);
 #pragma unroll 1
-    for (int r = wave; r < rows; r += 4) {
-      float x[D / 64], qm = 0.0f, sum = 0.0f;
-      x[0] = bf16_lo(next);
-      if constexpr (D == 128) x[1] = bf16_hi(next);
-      if (r + 4 < rows) fetch(r + 4);
-      if (a.k_had) rotate_wave<D>(x, lane);
+    for (int r0 = NG * wave; r0 < rows; r0 += 4 * NG) {
+      const int r = r0 + g8;
+      float x[8] = {bf16_lo(next.x), bf16_hi(next.x), bf16_lo(next.y), bf16_hi(next.y),
+                    bf16_lo(next.z), bf16_hi(next.z), bf16_lo(next.w), bf16_hi(next.w)};
+      if (r0 + 4 * NG < rows) fetch(r + 4 * NG);
+      if (a.k_had) {
+        fwht_lanes<LPH>(x, l8);
 #pragma unroll
-      for (int e = 0; e < D / 64; ++e) qm = fmaxf(qm, fabsf(x[e]));
-      qm = wave_max(qm);
-      const int e15 = 15 - __builtin_amdgcn_frexp_expf(qm);  // the row's largest in [2^14, 2^15)
-#pragma unroll
-      for (int e = 0; e < D / 64; ++e) {
-        const int d = lane * (D / 64) + e, f = d & 7;
-        const _Float16 h = (_Float16)__builtin_amdgcn_ldexpf(x[e], f & 1 ? e15 - 4 : e15);
-        u.q[r][(d & ~7) + (f < 4 ? 2 * f : 2 * f - 7)] = h;
-        sum += f & 1 ? 16.0f * (float)h : (float)h;
+        for (int i = 0; i < 8; ++i) x[i] *= hadamard_norm<D>();
       }
-      sum = wave_sum(sum);
-      // scores in the log2 domain: dots carry 2^(e15 - 24), sums of q 2^e15
-      if (lane == 0) {
-        s_qsum[r] = __builtin_amdgcn_ldexpf(sum, -24);
-        s_slope[r] = __builtin_amdgcn_ldexpf(a.sm_scale * LOG2E, 24 - e15);
+      float qm = 0.0f, sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) qm = fmaxf(qm, fabsf(x[i]));
+      qm = group_reduce<LPH>(qm, [](float p, float q) { return fmaxf(p, q); });
+      const int e15 = 15 - __builtin_amdgcn_frexp_expf(qm);  // the row's largest in [2^14, 2^15)
+      uint32_t word[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {  // channels k and k + 4, the odd ones / 16
+        const int e = k & 1 ? e15 - 4 : e15;
+        const h2_t h = {(_Float16)__builtin_amdgcn_ldexpf(x[k], e), (_Float16)__builtin_amdgcn_ldexpf(x[k + 4], e)};
+        const float both = (float)h.x + (float)h.y;
+        sum += k & 1 ? 16.0f * both : both;
+        word[k] = __builtin_bit_cast(uint32_t, h);
+      }
+      sum = group_reduce<LPH>(sum, [](float p, float q) { return p + q; });
+      if (r < rows) {
+        *reinterpret_cast<uint4*>(&u.q[r][8 * l8]) = make_uint4(word[0], word[1], word[2], word[3]);
+        // scores in the log2 domain: dots carry 2^(e15 - 24), sums of q 2^e15
+        if (l8 == 0) {
+          s_qsum[r] = __builtin_amdgcn_ldexpf(sum, -24);
+          s_slope[r] = __builtin_amdgcn_ldexpf(a.sm_scale * LOG2E, 24 - e15);
+        }
       }
     }
     for (int i = 64 * wave + lane; i < (16 * RT - rows) * (D / 8); i += 256)
@@ -360,7 +371,8 @@ kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, 
   auto compute = [&](int k0, const Block<D>& x) {
     // ---- the positions' parameters, by one lane each
     const int key = k0 + lane;
-    const bool valid = lane < 32 && ((x.ok >> (lane >> 4)) & 1) && key < k_stop;
+    // (no branch here: behind one, the wait for the parameters takes in the next block's loads)
+    const bool valid = (lane < 32) & ((x.ok >> (lane >> 4 & 1)) & 1) & (key < k_stop);
     const uint32_t vm = (uint32_t)__builtin_amdgcn_ballot_w64(valid);
     const float sk = valid ? fp16_bits_to_f32((uint16_t)x.par.x) : 0.0f;
     const float zk = valid ? (float)(int16_t)(x.par.x >> 16) : 0.0f;
@@ -490,10 +502,12 @@ kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, 
     }
   };
 
+  const int k_last = k_begin + ((k_stop - 1 - k_begin) & ~31);
   for (int k0 = k_begin; k0 < k_stop; k0 += 64) {
-    // (the ids of the block after this pair: a lane for each 16 positions, 1024 in all)
+    // (Past the end the last block again: behind a branch around the loads, the waits for the block
+    // before would take them in.  Page ids: a lane for each 16 positions, 1024 in all.)
     auto next = [&](int k, Block<D>& x) {
-      if (k >= k_stop) return;
+      k = min(k, k_last);
       if (k - id0 >= 1024) {
         id0 = k;
         ids = load_ids(id0);
@@ -545,26 +559,41 @@ kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, 
       }
     }
     __syncthreads();
-    for (int i = wave; i < 16 && 16 * t + i < rows; i += 4) {
-      const int row = 16 * t + i;
-      float ov[D / 64];
+    const int i = NG * wave + g8, row = 16 * t + i;
+    if (i < 16 && row < rows) {
+      float y[8] = {};
 #pragma unroll
-      for (int e = 0; e < D / 64; ++e) {
-        const int d = lane * (D / 64) + e;
-        ov[e] = (u.o[0][i][d] + u.o[1][i][d]) + (u.o[2][i][d] + u.o[3][i][d]);
-      }
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int c = 0; c < 8; c += 4) {
+          const float4 v = *reinterpret_cast<const float4*>(&u.o[k][i][8 * l8 + c]);
+          y[c] += v.x;
+          y[c + 1] += v.y;
+          y[c + 2] += v.z;
+          y[c + 3] += v.w;
+        }
       const float top = fmaxf(fmaxf(s_m[0][row], s_m[1][row]), fmaxf(s_m[2][row], s_m[3][row]));
       float lt = 0.0f;
 #pragma unroll
       for (int k = 0; k < 4; ++k) lt = __builtin_fmaf(s_l[k][row], __builtin_amdgcn_exp2f(s_m[k][row] - top), lt);
-      if (w.nchunk == 1) {
-        store_row<D>(a, w.s.q0 + row / G, hk * G + row % G, ov, lt, lane);
+      if (w.nchunk == 1) {  // (as in store_row)
+        const float f = lt == 0.0f ? 0.0f : 1.0f / lt;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) y[c] *= f;
+        if (a.v_had) {
+          fwht_lanes<LPH>(y, l8);
+#pragma unroll
+          for (int c = 0; c < 8; ++c) y[c] *= hadamard_norm<D>();
+        }
+        *reinterpret_cast<uint4*>(a.out + (int64_t)(w.s.q0 + row / G) * a.ldo + (int64_t)(hk * G + row % G) * D +
+                                  8 * l8) = make_uint4(bf16x2_rne(y[0], y[1]), bf16x2_rne(y[2], y[3]),
+                                                       bf16x2_rne(y[4], y[5]), bf16x2_rne(y[6], y[7]));
       } else {
         float* dst = rec + (int64_t)unit * few_rows * (D + 2);
-        if (lane == 0) *reinterpret_cast<float2*>(dst + 2 * row) = make_float2(top, lt);
-        dst += 2 * few_rows + row * D;
-        if constexpr (D == 128) reinterpret_cast<float2*>(dst)[lane] = make_float2(ov[0], ov[1]);
-        else dst[lane] = ov[0];
+        if (l8 == 0) *reinterpret_cast<float2*>(dst + 2 * row) = make_float2(top, lt);
+        dst += 2 * few_rows + row * D + 8 * l8;
+#pragma unroll
+        for (int c = 0; c < 8; c += 2) *reinterpret_cast<float2*>(dst + c) = make_float2(y[c], y[c + 1]);
       }
     }
     __syncthreads();
