@@ -210,9 +210,8 @@ __device__ __forceinline__ void store_row(const PagedAttentionArgs& a, int row, 
   else dst[lane] = f32_to_bf16_rne(o[0]);
 }
 
-// W: workgroups of a CU, waves of a SIMD.
-template <int D, int RT, int W>
-__global__ __launch_bounds__(256, W) void
+template <int D, int RT>
+__global__ __launch_bounds__(256, 2) void
 kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, int slots,
                               int chunk_min, const Plan* __restrict__ plan,
                               Joint* __restrict__ joints, float* __restrict__ rec) {
@@ -1445,7 +1444,7 @@ namespace {
 // tiles of the other kernel and over how many workgroups the keys of each are split.
 struct Shape {
   bool few, many, few_join, plan;
-  int few_rows, row_tiles, per_cu, units;
+  int few_rows, row_tiles, slots, units;
   int64_t tiles;
   int splits;
 };
@@ -1462,14 +1461,12 @@ Shape attention_shape(int64_t M, int64_t B, int64_t Hq, int64_t Hkv, int D, int6
   f.few = !f.many || B > 1;  // a single sequence of many rows: one launch
   f.row_tiles = f.many || most <= 16 ? 1 : most <= 32 ? 2 : most <= 48 ? 3 : 4;
   f.few_rows = f.few ? (int)(f.many ? 16 : most) : 0;
-  // Three workgroups a CU where the registers do (one row tile of 64 channels: 32 x 8000 positions
-  // 41 us, with two 46), and for 128 channels, where two spill nothing, when there are many rounds
-  // of short chunks: one token after 1024 x 300 positions 127 us, with two 154; 512 x 500 99 and
-  // 110; 8 x 32768 with 32 heads 211 and 205.
-  f.per_cu = f.row_tiles == 1 && (D == 64 || B * Hkv > 1024) ? 3 : 2;
+  // Chunks for two workgroups a CU, or for three where they are the lightest (32 x 8000 positions of
+  // 64 channels 41 us, for two 46; 8 x 32768 with 32 heads of 128 channels 211, for two 206).
+  f.slots = f.row_tiles == 1 && D == 64 ? 768 : 512;
   f.few_join = f.few && cap > CHUNK_ONE;
   f.plan = B > 64;
-  f.units = (int)((f.few_join ? 2 * 256 * f.per_cu : 0) + B * Hkv);
+  f.units = (int)((f.few_join ? 2 * f.slots : 0) + B * Hkv);
   f.splits = 1;
   if (f.many) {
     // (a sequence of r rows has ceil(r / ROWS) tiles)
@@ -1514,24 +1511,23 @@ hipError_t launch_kv_attention_paged(const PagedAttentionArgs& a, const PagedCac
   const int chunk_min = f.few_join ? CHUNK_MIN : CHUNK_ONE;
   if (plan)
     hipLaunchKernelGGL(kv_attention_paged_plan_kernel, dim3(1), dim3(1024), 0, stream, a, c.log2p, c.Hkv,
-                       f.few_rows, 256 * f.per_cu, chunk_min, plan, joints, starts);
+                       f.few_rows, f.slots, chunk_min, plan, joints, starts);
   FewJoin few = {};
   TileJoin tile = {};
   if (f.few) {
     float* rec = few_at + 4 * (int64_t)a.B;
-#define OFFQ_FEW(D_, RT_, W_)                                                                         \
-  hipLaunchKernelGGL((kv_attention_paged_few_kernel<D_, RT_, W_>), dim3((unsigned)f.units), dim3(256), \
-                     0, stream, a, c, f.few_rows, 256 * W_, chunk_min, plan, joints, rec)
+#define OFFQ_FEW(D_, RT_)                                                                        \
+  hipLaunchKernelGGL((kv_attention_paged_few_kernel<D_, RT_>), dim3((unsigned)f.units), dim3(256), \
+                     0, stream, a, c, f.few_rows, f.slots, chunk_min, plan, joints, rec)
     if (head_dim == 128) {
-      if (f.row_tiles == 1 && f.per_cu == 3) OFFQ_FEW(128, 1, 3);
-      else if (f.row_tiles == 1) OFFQ_FEW(128, 1, 2);
-      else if (f.row_tiles == 2) OFFQ_FEW(128, 2, 2);
-      else OFFQ_FEW(128, 3, 2);
+      if (f.row_tiles == 1) OFFQ_FEW(128, 1);
+      else if (f.row_tiles == 2) OFFQ_FEW(128, 2);
+      else OFFQ_FEW(128, 3);
     } else {
-      if (f.row_tiles == 1) OFFQ_FEW(64, 1, 3);
-      else if (f.row_tiles == 2) OFFQ_FEW(64, 2, 2);
-      else if (f.row_tiles == 3) OFFQ_FEW(64, 3, 2);
-      else OFFQ_FEW(64, 4, 2);
+      if (f.row_tiles == 1) OFFQ_FEW(64, 1);
+      else if (f.row_tiles == 2) OFFQ_FEW(64, 2);
+      else if (f.row_tiles == 3) OFFQ_FEW(64, 3);
+      else OFFQ_FEW(64, 4);
     }
 #undef OFFQ_FEW
     if (f.few_join) few = FewJoin{joints, rec, f.few_rows, f.few_rows * c.Hkv * a.B};
