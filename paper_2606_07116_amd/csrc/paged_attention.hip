@@ -1345,49 +1345,51 @@ struct TileJoin {
   int splits, blocks;
 };
 
-// Joins the chunks of a row: one workgroup per (sequence, key/value head, row), four waves over
-// the chunks.
+// Joins the chunks of a row: one workgroup per (sequence, key/value head, row), a chunk to each of
+// four waves in turn.  A chain of loads, each behind the one before; the lengths and the joint go
+// together.
 template <int D>
 __device__ __forceinline__ void join_chunks(const PagedAttentionArgs& a, int Hkv, int log2p,
                                             const FewJoin& w, int id) {
-  __shared__ float s_o[4][D], s_ml[2][4];
+  __shared__ float s_o[4][D];
   const int lane = (int)__builtin_amdgcn_workitem_id_x() & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)__builtin_amdgcn_workitem_id_x() >> 6);
   const int G = a.Hq / Hkv;
   const int hk = id % Hkv, row = id / Hkv % w.rows, b = id / Hkv / w.rows;
+  const Joint j = w.joints[b];  // (not written where the sequence has no chunks)
   const Seq s = sequence(a, log2p, G, b);
-  if (row >= s.rows || s.rows > w.rows) return;
-  const Joint j = w.joints[b];
-  if (j.nchunk <= 1) return;
+  if ((row >= s.rows) | (s.rows > w.rows) | (j.nchunk <= 1)) return;
   const int64_t size = (int64_t)w.rows * (D + 2);
   const float* first = w.rec + (int64_t)(j.unit0 + hk * j.nchunk) * size;
-  float top = LOWEST;
-  for (int i = lane; i < j.nchunk; i += 64) top = fmaxf(top, first[i * size + 2 * row]);
+  auto max_sum = [&](int i) {
+    return i < j.nchunk ? *reinterpret_cast<const float2*>(first + i * size + 2 * row) : make_float2(LOWEST, 0.0f);
+  };
+  float2 ml = max_sum(lane);
+  float top = ml.x;
+  for (int i = 64 + lane; i < j.nchunk; i += 64) top = fmaxf(top, max_sum(i).x);
   top = wave_max(top);
   float l = 0.0f, o[D / 64] = {};
-  for (int i0 = 64 * wave; i0 < j.nchunk; i0 += 256) {
-    float f = 0.0f;
-    if (i0 + lane < j.nchunk) {
-      const float2 ml = *reinterpret_cast<const float2*>(first + (i0 + lane) * size + 2 * row);
-      f = __builtin_amdgcn_exp2f(ml.x - top);
-      l = __builtin_fmaf(f, ml.y, l);
-    }
+  for (int i0 = 0; i0 < j.nchunk; i0 += 64) {
+    if (i0) ml = max_sum(i0 + lane);
+    const float f = __builtin_amdgcn_exp2f(ml.x - top);
+    l = __builtin_fmaf(f, ml.y, l);
     const int n = min(64, j.nchunk - i0);
     const float* src = first + i0 * size + 2 * w.rows + row * D + lane * (D / 64);
-    for (int k = 0; k < n; k += 8) {  // (factors past the last chunk are 0)
+    for (int k = wave; k < n; k += 32) {  // (factors past the last chunk are 0)
       float v[8][D / 64];
 #pragma unroll
       for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int e = 0; e < D / 64; ++e) v[i][e] = src[min(k + i, n - 1) * size + e];
+        for (int e = 0; e < D / 64; ++e) v[i][e] = src[min(k + 4 * i, n - 1) * size + e];
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
+      for (int i = 0; i < 8; ++i) {
+        const float fk = __shfl(f, k + 4 * i);
 #pragma unroll
-        for (int e = 0; e < D / 64; ++e) o[e] = __builtin_fmaf(__shfl(f, k + i), v[i][e], o[e]);
+        for (int e = 0; e < D / 64; ++e) o[e] = __builtin_fmaf(k + 4 * i < n ? fk : 0.0f, v[i][e], o[e]);
+      }
     }
   }
   l = wave_sum(l);
-  if (lane == 0) s_ml[0][wave] = l;
 #pragma unroll
   for (int e = 0; e < D / 64; ++e) s_o[wave][lane * (D / 64) + e] = o[e];
   __syncthreads();
@@ -1397,7 +1399,6 @@ __device__ __forceinline__ void join_chunks(const PagedAttentionArgs& a, int Hkv
     const int d = lane * (D / 64) + e;
     o[e] = (s_o[0][d] + s_o[1][d]) + (s_o[2][d] + s_o[3][d]);
   }
-  l = (s_ml[0][0] + s_ml[0][1]) + (s_ml[0][2] + s_ml[0][3]);
   store_row<D>(a, j.q0 + row / G, hk * G + row % G, o, l, lane);
 }
 
@@ -1418,10 +1419,18 @@ __device__ __forceinline__ void join_splits(const PagedAttentionArgs& a, int Hkv
   const float l = wave_sum(f * ml.y);
   float o[D / 64] = {};
   src += 2 * ROWS + i * D + lane * (D / 64);
-  for (int k = 0; k < j.nsplit; ++k) {
-    const float fk = __shfl(f, k);
+  for (int k = 0; k < j.nsplit; k += 4) {
+    float v[4][D / 64];
 #pragma unroll
-    for (int e = 0; e < D / 64; ++e) o[e] = __builtin_fmaf(fk, src[k * size + e], o[e]);
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int e = 0; e < D / 64; ++e) v[q][e] = src[min(k + q, j.nsplit - 1) * size + e];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float fk = __shfl(f, k + q);
+#pragma unroll
+      for (int e = 0; e < D / 64; ++e) o[e] = __builtin_fmaf(k + q < j.nsplit ? fk : 0.0f, v[q][e], o[e]);
+    }
   }
   const int G = a.Hq / Hkv, row = j.row0 + i;
   store_row<D>(a, j.q0 + row / G, hk * G + row % G, o, l, lane);
