@@ -69,10 +69,10 @@ __device__ __forceinline__ Seq sequence(const PagedAttentionArgs& a, int log2p, 
 // weights by one that follows the largest value scale met.
 //
 // Measured (a large copy here: 4.9 TB/s, reads alone 6.2): 8 x 32768 positions of 32 heads of their
-// own 205 us, 5.5 TB/s; 24 ragged sequences of up to 30000, five query heads to each of 8, 75 us
-// with the join's 5; 16 x 4097 22 us for 71 MB.  A workgroup costs 6 us besides its positions'
+// own 205 us, 5.6 TB/s; 24 ragged sequences of up to 30000, five query heads to each of 8, 70 us
+// with the join's 5; 16 x 4097 21 us for 72 MB.  A workgroup costs 6 us besides its positions'
 // bytes (who it is, page ids, first block, queries, the waves' join), which is what is left there
-// and below: one token after 300 positions 8.4 us.
+// and below: one token after 300 positions 8.3 us.
 struct Chunking {
   int len;          // positions per chunk, a multiple of 128
   int b, head, chunk, nchunk, unit0;  // this unit's; unit0: the sequence's first unit
@@ -1463,9 +1463,9 @@ Shape attention_shape(int64_t M, int64_t B, int64_t Hq, int64_t Hkv, int D, int6
   Shape f = {};
   // The few-row kernel takes codes straight into its operands, which costs the least per position,
   // but its time grows with the row tiles, and at 64 rows of 128 channels it runs out of
-  // registers: 8 new tokens of 8 heads, 4 x 5000 positions: 92 us there, 46 us as a tile that is
-  // three quarters empty; 5 tokens: 46 both, 334 and 377 us with 64 x 5000.  64 rows of 64
-  // channels: 32 us there, 51 us as a tile.
+  // registers: 8 new tokens of 8 heads, 4 x 5000 positions: 92 us there, 36 us as a tile that is
+  // three quarters empty; 5 tokens 36 us there, 38 as a tile, with 64 x 5000 241 and 334.  64 rows
+  // of 64 channels: 32 us there, 51 us as a tile.
   f.many = most > (D == 128 ? 48 : 64);
   f.few = !f.many || B > 1;  // a single sequence of many rows: one launch
   f.row_tiles = f.many || most <= 16 ? 1 : most <= 32 ? 2 : most <= 48 ? 3 : 4;

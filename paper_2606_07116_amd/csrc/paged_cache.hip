@@ -12,10 +12,10 @@
 // Read: s (c - z), then c H of it where asked, rounded to bf16 once.
 //
 // Both are bound by memory where they are large (a large copy here: 4.9 TB/s).  Write, 8191 tokens
-// of 48 heads with norms: 42 us for 176 MB, 4.2 TB/s, its vector work 70 % of that; angles from
-// LDS for each unit, a hardware reciprocal root, six to eight waves per SIMD and a second unit on
-// its way did not change it.  Read, 131072 rows of 8 heads: 152 us for 680 MB, 4.5 TB/s.  Below
-// about 1000 rows a call is its launch, 4 us.
+// of 48 heads with norms: 39 us for 176 MB, 4.5 TB/s, its vector work 75 % of that; angles from
+// LDS for each round, a hardware reciprocal root, eight waves per SIMD and a second round on its
+// way did not change it.  Read, 131072 rows of 8 heads: 152 us for 680 MB, 4.5 TB/s.  Below about
+// 1000 rows a call is its launch, 4 us.
 #include <type_traits>
 
 #include "internal.h"
