@@ -471,6 +471,7 @@ offq_status_t offq_rope_inv_freq(int32_t rotary_dim, double base, double factor,
  *   slots      int64 [M]: where token m's rows go; a slot outside
  *              [0, num_pages * page_size) writes nothing to the cache.  Two tokens
  *              of a call with the same slot leave its content unspecified.
+ * M <= 2^26 - 4.
  */
 offq_status_t offq_rope_kv_paged(const uint16_t* qkv, int64_t ldq, int64_t M, int64_t Hq, int64_t Hkv,
                        int32_t head_dim, const uint16_t* q_weight, const uint16_t* k_weight,
@@ -488,6 +489,7 @@ offq_status_t offq_rope_kv_paged(const uint16_t* qkv, int64_t ldq, int64_t M, in
  *              [0, num_pages * page_size) are left as they were.
  *   k_out, v_out  bf16 [M, Hkv D], row strides ldk, ldv (multiples of 8),
  *              16-byte aligned; either may be NULL (not both).
+ * M Hkv D < 2^35.
  */
 offq_status_t offq_kv_dequantize_paged(const uint8_t* k_codes, const uint8_t* v_codes,
                              const int16_t* kv_params, int64_t num_pages, int32_t page_size,
@@ -521,7 +523,7 @@ offq_status_t offq_kv_dequantize_paged(const uint8_t* k_codes, const uint8_t* v_
  *              max_new) bytes, 16-byte aligned (NULL where that is 0); scratch.
  *              Calls that share a workspace must be ordered on one stream.
  * Lengths and tables are read on the device only, so that a captured call
- * replays with new ones.
+ * replays with new ones.  M <= 2^24, M Hq <= 2^30, Hq <= 4096, B Hkv < 2^18.
  */
 offq_status_t offq_kv_attention_paged(const uint16_t* q, int64_t ldq, int64_t M, int64_t Hq, int64_t Hkv,
                             int32_t head_dim, const int32_t* q_starts, const int32_t* seq_lens,

@@ -619,3 +619,93 @@ def test_rows_far_larger_than_their_neighbours(new, past):
         got = _attend(new, past, 4, 2, 128, 16, seed=18, spoil=spoil)[2]
         if not math.isfinite(value):
             assert np.isnan(got[5, 1]).all() and np.isfinite(got[5, 0]).all()
+
+
+def _mixed_call(rng, B, new, past, D=128, Hq=8, Hkv=2, P_=16):
+    """Device operands of an attention call over a cache of random rows."""
+    lens = [n + p for n, p in zip(new, past)]
+    table, pages = _tables(rng, lens, P_, width=-(-max(lens) // P_) + 40)
+    q = torch.randn((sum(new), Hq, D), device=DEV).bfloat16()
+    starts = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    return [q, _t(starts), _t(np.array(lens, np.int32)), _t(table),
+            _cache(*_host_cache(rng, pages, Hkv, P_, D))]
+
+
+def test_two_graphs_share_a_workspace_and_take_new_lengths():
+    """Replays in turn, with other lengths and other rows per sequence each time, against eager
+    calls with a workspace of their own."""
+    rng = np.random.default_rng(20)
+    torch.manual_seed(20)
+    new = [1] * 60 + [0, 3, 40, 1, 0, 70, 1, 2, 90, 1]
+    calls = [_mixed_call(rng, 70, new, rng.integers(0, 900, 70).tolist()),
+             _mixed_call(rng, 3, [300, 2, 1], [1500, 30, 5000])]
+    most = [90, 300]
+    need = [offq.offq_kv_attention_paged_workspace_bytes(c[0].shape[0], c[2].shape[0], 8, 2, 128, m)
+            for c, m in zip(calls, most)]
+    ws = torch.full((max(need),), 255, dtype=torch.uint8, device=DEV)
+    outs = [torch.empty_like(c[0]) for c in calls]
+    graphs = []
+    for c, m, o in zip(calls, most, outs):
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            offq.offq_kv_attention_paged(*c, m, out=o, workspace=ws)
+        torch.cuda.current_stream().wait_stream(s)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            offq.offq_kv_attention_paged(*c, m, out=o, workspace=ws)
+        graphs.append(g)
+    full = [c[2].clone() for c in calls]
+    first = calls[0][1].clone()
+    for turn in range(5):
+        for i in (0, 1) if turn % 2 else (1, 0):
+            c = calls[i]
+            c[2].copy_((full[i] - 7 * turn * (i + 1)).clamp(min=0))
+            if i == 0 and turn == 2:  # the rows go to the last sequences instead
+                lens = (first[1:] - first[:-1]).flip(0)
+                c[1][1:] = torch.cumsum(lens, 0).int()
+            outs[i].fill_(5.0)
+            graphs[i].replay()
+            got = outs[i].clone()
+            want = offq.offq_kv_attention_paged(*c, most[i], out=torch.full_like(c[0], 5.0))
+            torch.cuda.synchronize()
+            assert torch.equal(got, want), (turn, i)
+
+
+def test_two_streams_at_once():
+    rng = np.random.default_rng(21)
+    torch.manual_seed(21)
+    calls = [(_mixed_call(rng, 80, [1] * 80, rng.integers(0, 2000, 80).tolist()), 1),
+             (_mixed_call(rng, 2, [400, 9], [700, 3000]), 400)]
+    want = [offq.offq_kv_attention_paged(*c, m) for c, m in calls]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    got = [[], []]
+    for _ in range(4):
+        for s, (c, m), g in zip(streams, calls, got):
+            with torch.cuda.stream(s):
+                g.append(offq.offq_kv_attention_paged(*c, m))
+    torch.cuda.synchronize()
+    for w, g in zip(want, got):
+        assert all(torch.equal(w, x) for x in g)
+
+
+def test_write_and_read_same_rows_again():
+    """Slots read twice, in any order; a write of tokens without a slot leaves the cache."""
+    torch.manual_seed(22)
+    cache = offq.paged_cache(4, 3, 16, 64, device=DEV)
+    x = torch.randn((64, (6 + 6) * 64), device=DEV).bfloat16()
+    pos = torch.arange(64, dtype=torch.int32, device=DEV)
+    slots = torch.randperm(64, device=DEV)
+    f = offq.offq_rope_inv_freq(64, device=DEV)
+    offq.offq_rope_kv_paged(x, 6, pos, slots, cache, f)
+    keep = {n: t.clone() for n, t in cache.items()}
+    q = offq.offq_rope_kv_paged(x, 6, pos, torch.full_like(slots, -1), cache, f)
+    again = torch.cat([slots[:9], slots[:9].flip(0), slots[3:4].repeat(20)])
+    k, v = offq.offq_kv_dequantize_paged(cache, again)
+    k1, v1 = offq.offq_kv_dequantize_paged(cache, slots)
+    torch.cuda.synchronize()
+    assert all(torch.equal(cache[n], keep[n]) for n in cache)
+    at = torch.cat([torch.arange(9), torch.arange(9).flip(0), torch.full((20,), 3)])
+    assert torch.equal(k, k1[at.to(DEV)]) and torch.equal(v, v1[at.to(DEV)])
+    assert q.isfinite().all()
