@@ -1475,7 +1475,10 @@ Shape attention_shape(int64_t M, int64_t B, int64_t Hq, int64_t Hkv, int D, int6
   f.slots = f.row_tiles == 1 && D == 64 ? 768 : 512;
   f.few_join = f.few && cap > CHUNK_ONE;
   f.plan = B > 64;
-  f.units = (int)((f.few_join ? 2 * f.slots : 0) + B * Hkv);
+  // (what the chunk length allows, and what the page table has room for)
+  const int64_t units = (f.few_join ? 2 * f.slots : 0) + B * Hkv;
+  const int64_t room = B * Hkv * (cap <= CHUNK_ONE ? 1 : (cap + CHUNK_MIN - 1) / CHUNK_MIN);
+  f.units = (int)(units < room ? units : room);
   f.splits = 1;
   if (f.many) {
     // (a sequence of r rows has ceil(r / ROWS) tiles)
