@@ -612,8 +612,9 @@ kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, 
 //   its own: A z_j and sum q as three fp16 pieces each, their six leading products;
 // * the score product starts from -m, the row's reference, so what it leaves are the exponents of
 //   the weights: per weight one exp2, half a conversion to fp16 and half a dot product for the
-//   sum.  That a reference has to move shows in the sum itself: infinite where a weight left the
-//   fp16 range, zero before the first position;
+//   sum.  A row takes its reference from the scores of the first tile that it sees, wherever they
+//   lie (left at 0, rows 2^-16 to 2^-25 below it lost their weights' bits to fp16's subnormals);
+//   that it has to move later shows in the sum, infinite where a weight left the fp16 range;
 // * S^T = K Q^T: a lane holds 16 positions of one query row per tile of 32, so maximum and sum
 //   stay in the lane, and the tile is in the operand layout of O^T = V^T P^T; V^T lies in LDS with
 //   the positions in the order of the accumulator and the channels as (nibble, code word), so
@@ -1131,10 +1132,10 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
       }
     }
   };
-  // After the weights of `s`: rows that met their first position, or a weight beyond the range,
-  // move their reference, also under the scores `t` that were formed meanwhile.
+  // After the weights of `s`: rows that had met no position before, or now a weight beyond the
+  // range, move their reference, also under the scores `t` that were formed meanwhile.
   auto settle = [&](f16_t& s, f16_t& t, float sum) {
-    if (__builtin_amdgcn_ballot_w64(!(sum > 0.0f && sum < HUGE_SUM))) {
+    if (__builtin_amdgcn_ballot_w64(!(l > 0.0f && sum < HUGE_SUM))) {
       float top = s[0];
 #pragma unroll
       for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);

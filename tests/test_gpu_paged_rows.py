@@ -1,0 +1,114 @@
+"""GPU: rows of the paged attention (offq_kv_attention_paged) in the company that they keep, and
+scores wherever they lie, against fp64 softmax over the values that the cache stands for.
+
+A softmax does not change when a row's scores all move by the same amount, and a row's result does
+not depend on positions that it does not see or on the rows beside it.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2606_07116_amd as offq
+from oracle import paged as OP
+from tests import parity as P
+from tests.test_gpu_paged import _bf16, _cache, _host_cache, _t, _tables
+
+pytestmark = pytest.mark.gpu
+
+DEV = P.DEV
+
+
+class Call:
+    """Sequences of new[b] rows after past[b] positions over a cache of random rows; `cache` and
+    `queries` change them before the call."""
+
+    def __init__(self, new, past, Hq=4, Hkv=2, D=128, P_=16, seed=0, cache=None, queries=None):
+        rng = np.random.default_rng(seed)
+        self.new, self.lens = new, [n + p for n, p in zip(new, past)]
+        self.table, pages = _tables(rng, self.lens, P_)
+        self.host = _host_cache(rng, pages, Hkv, P_, D)
+        self.starts = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+        self.q = _bf16(rng, sum(new), Hq, D)
+        if cache:
+            cache(self)
+        if queries:
+            queries(self.q)
+
+    def slot(self, b, j):
+        P_ = self.host[2].shape[2]
+        return self.table[b, j // P_], j % P_
+
+    def run(self, sm, k_had=True, v_had=False):
+        out = offq.offq_kv_attention_paged(
+            P.to_dev_bf16(self.q), _t(self.starts), _t(np.array(self.lens, np.int32)), _t(self.table),
+            _cache(*self.host), max(self.new), sm_scale=sm, k_hadamard=k_had, v_hadamard=v_had)
+        torch.cuda.synchronize()
+        return P.host(out.float()).astype(np.float64)
+
+    def exact(self, sm, k_had=True, v_had=False):
+        """fp64, all rows of a sequence at once."""
+        kc, vc, par = self.host
+        qr = OP.hadamard_rows(self.q, k_had)
+        out = np.zeros_like(qr)
+        G = qr.shape[1] // par.shape[1]
+        for b, n in enumerate(self.new):
+            slots = OP.sequence_slots(self.table[b], self.lens[b], par.shape[2], par.shape[0])
+            at = np.flatnonzero(slots >= 0)
+            if not n or not len(at):
+                continue
+            K = OP.dequantize(kc, par, slots[at])
+            V = OP.dequantize(vc, par, slots[at], value=True)
+            see = at <= self.lens[b] - n + np.arange(n)[:, None]
+            rows = slice(self.starts[b], self.starts[b + 1])
+            for h in range(qr.shape[1]):
+                s = np.where(see, sm * (qr[rows, h] @ K[:, h // G].T), -np.inf)
+                top = s.max(-1, keepdims=True)
+                p = np.where(see, np.exp(s - np.where(np.isfinite(top), top, 0)), 0)
+                out[rows, h] = (p / np.maximum(p.sum(-1, keepdims=True), 1e-300)) @ \
+                    np.where(see.any(0)[:, None], V[:, h // G], 0)
+        return OP.hadamard_rows(out, v_had)
+
+
+def _error(got, ref):
+    """The error's norm over the output's."""
+    return math.sqrt(((got - ref) ** 2).sum() / (ref ** 2).sum())
+
+
+# ------------------------------------------------------------------ scores anywhere
+# log2 of what every weight loses; sm_scale sk sqrt(D) q_0 log2(e) is 1/4 per step of the zero-point
+DROPS = [0, 8, 12, 16, 18, 20, 22, 23, 24, 25, 26, 40]
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("new,past,absent", [
+    ([300], [0], 0), ([150, 1, 64], [0, 90, 40], 0), ([70], [3000], 0), ([3, 40], [900, 1500], 0),
+    ([90], [700], 9), ([5], [400], 2), ([1, 4], [1300, 20], 0),
+])
+def test_scores_below_zero(new, past, absent, D):
+    """Keys moved along the first channel of the unrotated queries, which all rows share: every
+    score of a row drops by the same amount and the outputs stay.  (The same errors to a half: the
+    roundings of the scores' terms grow with the offset, 2^-11 of up to 40 / ln 2, those of the
+    queries and codes that differ from row to row do not.)"""
+    sm = 0.25 / (math.log2(math.e) * 0.125 * math.sqrt(D) * 2)
+
+    def offset(by):
+        def change(call):
+            par = call.host[2]
+            par[..., 0] = np.float16(0.125).view(np.int16)
+            par[..., 1] = 7 + by
+            call.table[:, :absent] = -1
+        return change
+
+    def first(q):
+        q[..., 0] = 2.0
+
+    errors = {}
+    for drop in DROPS:
+        call = Call(new, past, D=D, seed=sum(new) + D, cache=offset(4 * drop), queries=first)
+        errors[drop] = _error(call.run(sm), call.exact(sm))
+    print(" ".join(f"{d}: {e:.5f}" for d, e in errors.items()))
+    # bf16 outputs alone leave between 2^-8 / 4 and 2^-8 / sqrt(3)
+    assert errors[0] <= 2.0 ** -8
+    assert max(errors.values()) <= 1.5 * errors[0], errors
