@@ -605,9 +605,13 @@ kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, 
 // key the products bound it, so both run as 32x32x16 fp16 matrix products and everything that
 // can leave the score loop does:
 // * a block's codes become fp16 values once per workgroup, on their way to LDS: keys A c with
-//   A = sk 2^-E, values A (c - z) with A = sv 2^-F, one rounding each (2^-11; a value's zero-point
-//   term another).  E and F are the workgroup's and follow the largest sk (8192 + |z|) and
-//   sv (16 + |z|) met, rarely; the query carries sm_scale log2(e) 2^E;
+//   A = sk 2^-E, values A (c - z') with A = sv 2^-F and z' the zero-point held in 0 .. 15, one
+//   rounding each (2^-11; a value's zero-point term another).  E and F are the workgroup's and
+//   follow the largest sk (8192 + |z|) and sv met, rarely; the query carries sm_scale log2(e) 2^E;
+// * what a value's zero-point has beyond its codes, A (z - z'), is one number a row and stays in
+//   fp32: blocks that have any, a flag of theirs, sum the weights times it, in the branch that
+//   moves references (in fp16, offsets of 300 and 3000 steps left noise of 1.3 and 12 % of their
+//   norm in the other channels of values that are rotated back);
 // * the keys' zero-point term -z_j sum q, which can be far larger than the score, is a k-step of
 //   its own: A z_j and sum q as three fp16 pieces each, their six leading products;
 // * the score product starts from -m, the row's reference, so what it leaves are the exponents of
@@ -646,8 +650,9 @@ struct alignas(16) Stage {
   struct Par {                      // what a block's codes are staged with
     uint4 z[KB];                    // per position: the pieces of the keys' A z 2^-13
     uint32_t a[KB];                 // the keys' A and A / 16
-    uint32_t ab[KB];                // the values' A and -A z 2^-9
-    int E, F;
+    uint32_t ab[KB];                // the values' A and -A z' 2^-9
+    float rest[KB];                 // the values' A (z - z') 2^-9
+    int E, F;                       // (F of values, twice, and whether any `rest` is not 0)
     uint32_t valid[2];              // bit j: position j is there
   } par[4];
 };
@@ -926,15 +931,16 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
     const Pieces u = pieces(ka * zk * 0x1p-13f);
     P.z[lane] = make_uint4(pk_f16(u.h1, u.h1), pk_f16(u.h2, u.h1), pk_f16(u.h2, u.h3), 0);
     P.a[lane] = pk_f16(ka, ka * 0.0625f);
-    // values: A (16 + |z|) stays below 2^19
-    const float vt = wave_max(sv * (16.0f + fabsf(zv)));
-    if (vt > 0.0f) F = max(F, __builtin_amdgcn_frexp_expf(vt) - 19);
-    const float va = __builtin_amdgcn_ldexpf(sv, -F);
-    P.ab[lane] = pk_f16(va, -va * zv * 0x1p-9f);
-    const uint64_t vm = __builtin_amdgcn_ballot_w64(ok);
+    // values: A stays below 2^15
+    const float vt = wave_max(sv);
+    if (vt > 0.0f) F = max(F, __builtin_amdgcn_frexp_expf(vt) - 15);
+    const float va = __builtin_amdgcn_ldexpf(sv, -F), z = __builtin_amdgcn_fmed3f(zv, 0.0f, 15.0f);
+    P.ab[lane] = pk_f16(va, -va * z * 0x1p-9f);
+    P.rest[lane] = va * (zv - z) * 0x1p-9f;
+    const uint64_t vm = __builtin_amdgcn_ballot_w64(ok), far = __builtin_amdgcn_ballot_w64(sv != 0.0f && zv != z);
     if (lane == 0) {
       P.E = E;
-      P.F = F;
+      P.F = 2 * F + (far != 0);
       P.valid[0] = (uint32_t)vm;
       P.valid[1] = (uint32_t)(vm >> 32);
     }
@@ -1079,7 +1085,7 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
   f16_t neg;  // -m in every register: what the score products start from
 #pragma unroll
   for (int r = 0; r < 16; ++r) neg[r] = 0.0f;
-  float l = 0.0f;
+  float l = 0.0f, zsum = 0.0f;
   int Eq = E, Fo = -200;  // the scaling that the queries and the outputs carry
 
   // QK of a tile of 32 positions in slot `slot`.  The first operands of a product are read while
@@ -1132,10 +1138,16 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
       }
     }
   };
-  // After the weights of `s`: rows that had met no position before, or now a weight beyond the
-  // range, move their reference, also under the scores `t` that were formed meanwhile.
-  auto settle = [&](f16_t& s, f16_t& t, float sum) {
-    if (__builtin_amdgcn_ballot_w64(!(l > 0.0f && sum < HUGE_SUM))) {
+  // After the weights of `s`, tile tt of a block: rows that had met no position before, or now a
+  // weight beyond the range, move their reference, also under the scores `t` that were formed
+  // meanwhile; then the values' zero-points beyond their codes, where the block has any.
+  auto settle = [&](f16_t& s, f16_t& t, float sum, int kb, int tt, int far) {
+    const uint64_t moving = __builtin_amdgcn_ballot_w64(!(l > 0.0f && sum < HUGE_SUM));
+    if (!(moving | (uint64_t)far)) {
+      l = sum;
+      return;
+    }
+    if (moving) {
       float top = s[0];
 #pragma unroll
       for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
@@ -1145,6 +1157,7 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
       const float by = move ? top - MID : 0.0f;
       const float f = both == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(-by);
       l *= f;
+      zsum *= f;
 #pragma unroll
       for (int d = 0; d < ND; ++d) o[d] *= f;
 #pragma unroll
@@ -1156,6 +1169,16 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
       sum = weights(s, l);
     }
     l = sum;
+    if (far) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {  // registers 4 k .. 4 k + 3: positions 8 k + 4 h and on
+        const float4 z = *reinterpret_cast<const float4*>(&S.par[kb & 3].rest[32 * tt + 8 * k + 4 * h]);
+        const h2_t p = __builtin_bit_cast(h2_t, wb[k >> 1][2 * (k & 1)]);
+        const h2_t q = __builtin_bit_cast(h2_t, wb[k >> 1][2 * (k & 1) + 1]);
+        zsum = __builtin_fmaf((float)p.x, z.x, __builtin_fmaf((float)p.y, z.y, zsum));
+        zsum = __builtin_fmaf((float)q.x, z.z, __builtin_fmaf((float)q.y, z.w, zsum));
+      }
+    }
   };
   auto value_at = [&](int slot, int tt, int i) {
     return *reinterpret_cast<const uint4*>(S.v[slot] + (32 * (i % ND) + ql) * VROW +
@@ -1209,7 +1232,7 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
     // (keys, then values, as in the loop: the waits count the loads issued later)
     load_k(min(kb0 + 2, kbl));
     load_v(min(kb0 + 1, kbl));
-    auto meta = [&](int kb) {  // E, F, valid
+    auto meta = [&](int kb) {  // E, F and its flag, valid
       const int4 x = *reinterpret_cast<const int4*>(&S.par[kb & 3].E);
       return make_int4(uniform(x.x), uniform(x.y), uniform(x.z), uniform(x.w));
     };
@@ -1222,7 +1245,7 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
       load_v(min(kb + 2, kbl));
       if (((kb - kb0) & 7) == wave) {
         const int4 before = meta(kb + 2);
-        prepare(kb + 3, page0, par0, before.x, before.y);
+        prepare(kb + 3, page0, par0, before.x, before.y >> 1);
         page0 = page1;
         par0 = params(kb + 11, page0);
         page1 = page_of(kb + 19);
@@ -1247,17 +1270,19 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
     for (int kb = kb0; kb < kb1; ++kb) {
       const int sl1 = sl == 2 ? 0 : sl + 1, sl2 = sl1 == 2 ? 0 : sl1 + 1;
       const int4 next = meta(kb + 1);
-      if (now.y != Fo) {
-        const float f = __builtin_amdgcn_ldexpf(1.0f, max(Fo - now.y, -150));
+      const int F = now.y >> 1, far = now.y & 1;
+      if (F != Fo) {
+        const float f = __builtin_amdgcn_ldexpf(1.0f, max(Fo - F, -150));
+        zsum *= f;
 #pragma unroll
         for (int d = 0; d < ND; ++d) o[d] *= f;
-        Fo = now.y;
+        Fo = F;
       }
       mask(s0, kb * KB, (uint32_t)now.z);
       scores(sl, 1, s1);
       fetch_v(vs, 0);
       float sum = weights(s0, l);
-      settle(s0, s1, sum);
+      settle(s0, s1, sum, kb, 0, far);
       fetch_k(kb + 1, sl1, 0);
       values(vs, 0);
       stage_keys(kb, sl2);
@@ -1266,7 +1291,7 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
       scores(sl1, 0, s0);
       fetch_v(vs, 1);
       sum = weights(s1, l);
-      settle(s1, s0, sum);
+      settle(s1, s0, sum, kb, 1, far);
       fetch_k(kb + 1, sl1, 1);
       values(vs, 1);
       stage_values(kb, vs ^ 1);
@@ -1278,6 +1303,9 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
   }
   if (wrow > last) return;
   l += __shfl_xor(l, 32);
+  zsum += __shfl_xor(zsum, 32);
+#pragma unroll
+  for (int d = 0; d < ND; ++d) o[d] -= zsum;
   if (bad && l > 0.0f) l = __builtin_nanf("");
 
   // ---- channels: o[d][r] is channel 8 word + nibble of V^T's row 32 d + 8 (r / 4) + 4 h + r % 4

@@ -112,3 +112,26 @@ def test_scores_below_zero(new, past, absent, D):
     # bf16 outputs alone leave between 2^-8 / 4 and 2^-8 / sqrt(3)
     assert errors[0] <= 2.0 ** -8
     assert max(errors.values()) <= 1.5 * errors[0], errors
+
+
+# ------------------------------------------------------------------ values around an offset
+@pytest.mark.parametrize("offset", [40, -300, 3000, -30000])
+@pytest.mark.parametrize("new,past", [([300], [0]), ([70, 2], [1500, 300]), ([5], [300])])
+@pytest.mark.parametrize("D", [64, 128])
+def test_values_around_an_offset(offset, new, past, D):
+    """Rotated values whose zero-points are far from their codes: the offset is channel 0's alone
+    once the sum is rotated back, and the other channels keep their bits.  What they may lose: half
+    a bf16 step and the weights' and codes' fp16 roundings (1.5 x 2^-8 of their norm in all), and
+    the fp32 roundings of the offset, of the butterflies' L stages and the two steps before them:
+    sqrt(L + 2) 2^-24 / sqrt(3) of channel 0 as a norm, twice that allowed and rounded up, 2^-22."""
+    def shift(call):
+        rng = np.random.default_rng(1)
+        zero = call.host[2][..., 3]
+        zero[...] = 7 + offset + rng.integers(-3, 4, zero.shape)
+
+    call = Call(new, past, D=D, seed=abs(offset) + D, cache=shift)
+    got, ref = (f(1 / math.sqrt(D), v_had=True) for f in (call.run, call.exact))
+    off = np.linalg.norm((got - ref)[..., 1:])
+    print(off / np.linalg.norm(ref[..., 1:]))
+    assert off <= 1.5 * 2.0 ** -8 * np.linalg.norm(ref[..., 1:]) + 2.0 ** -22 * np.linalg.norm(ref[..., 0])
+    assert np.linalg.norm((got - ref)[..., 0]) <= 2.0 ** -8 * np.linalg.norm(ref[..., 0])
