@@ -617,14 +617,17 @@ kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, 
 // * the score product starts from -m, the row's reference, so what it leaves are the exponents of
 //   the weights: per weight one exp2, half a conversion to fp16 and half a dot product for the
 //   sum.  A row takes its reference from the scores of the first tile that it sees, wherever they
-//   lie (left at 0, rows 2^-16 to 2^-25 below it lost their weights' bits to fp16's subnormals);
-//   that it has to move later shows in the sum, infinite where a weight left the fp16 range;
+//   lie (left at 0, rows 2^-16 to 2^-25 below it lost their weights' bits to fp16's subnormals):
+//   before the loop where that is its workgroup's first tile.  That it has to move later shows in
+//   the sum, infinite where a weight left the fp16 range and, so far, for a row that saw nothing;
 // * S^T = K Q^T: a lane holds 16 positions of one query row per tile of 32, so maximum and sum
 //   stay in the lane, and the tile is in the operand layout of O^T = V^T P^T; V^T lies in LDS with
 //   the positions in the order of the accumulator and the channels as (nibble, code word), so
 //   that a lane ends with eight consecutive channels of each of its words;
-// * a moved reference puts the row's largest weight of that tile at 2^7: 2^9 below the range's
-//   end, and what lies 2^31 below it still counts.  The sum is taken of the rounded weights.
+// * a reference puts the row's largest weight of its tile at 2^3: 2^13 below the range's end, and
+//   what lies 2^27 below it still counts.  (At 2^7 the same instructions took 2 % longer, 674 us for
+//   656: small weights become subnormal and 0, and the clock is as high as the bits allow.)  The
+//   sum is taken of the rounded weights.
 // Longest tiles start first.  Where the tiles do not fill the CUs, the keys of a tile are split
 // over workgroups and the rows joined by a second kernel.
 //
@@ -638,7 +641,7 @@ kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, 
 constexpr int ROWS = 256;      // query rows of a tile
 constexpr int KB = 64;         // positions of a block
 constexpr int VROW = 2 * KB + 16;
-constexpr float MID = 7.0f;    // a reference that moves puts its row's largest weight at 2^MID
+constexpr float MID = 3.0f;    // a reference puts its row's largest weight of a tile at 2^MID
 constexpr float HUGE_SUM = 3e38f;
 
 typedef float f16_t __attribute__((ext_vector_type(16)));
@@ -1085,7 +1088,7 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
   f16_t neg;  // -m in every register: what the score products start from
 #pragma unroll
   for (int r = 0; r < 16; ++r) neg[r] = 0.0f;
-  float l = 0.0f, zsum = 0.0f;
+  float l = __builtin_inff(), zsum = 0.0f;  // (l: nothing seen)
   int Eq = E, Fo = -200;  // the scaling that the queries and the outputs carry
 
   // QK of a tile of 32 positions in slot `slot`.  The first operands of a product are read while
@@ -1138,25 +1141,28 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
       }
     }
   };
-  // After the weights of `s`, tile tt of a block: rows that had met no position before, or now a
-  // weight beyond the range, move their reference, also under the scores `t` that were formed
-  // meanwhile; then the values' zero-points beyond their codes, where the block has any.
+  auto row_max = [&](const f16_t& s) {
+    float top = s[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
+    return fmaxf(top, __shfl_xor(top, 32));
+  };
+  // After the weights of `s`, tile tt of a block: rows that had met no position before (an infinite
+  // l), or now a weight beyond the range, move their reference, also under the scores `t` that were
+  // formed meanwhile; then the values' zero-points beyond their codes, where the block has any.
   auto settle = [&](f16_t& s, f16_t& t, float sum, int kb, int tt, int far) {
-    const uint64_t moving = __builtin_amdgcn_ballot_w64(!(l > 0.0f && sum < HUGE_SUM));
+    const uint64_t moving = __builtin_amdgcn_ballot_w64(!(sum < HUGE_SUM));
     if (!(moving | (uint64_t)far)) {
       l = sum;
       return;
     }
     if (moving) {
-      float top = s[0];
-#pragma unroll
-      for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const float both = l + __shfl_xor(l, 32);
-      const bool move = top > -__builtin_inff() && (both == 0.0f || top > MID + 8.0f);
+      const float top = row_max(s);
+      const bool first = l == __builtin_inff();
+      const bool move = top > -__builtin_inff() && (first || top > MID + 8.0f);
       const float by = move ? top - MID : 0.0f;
-      const float f = both == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(-by);
-      l *= f;
+      const float f = __builtin_amdgcn_exp2f(first ? 0.0f : -by);  // (of a first one, o and zsum are 0)
+      l = first && move ? 0.0f : l * f;
       zsum *= f;
 #pragma unroll
       for (int d = 0; d < ND; ++d) o[d] *= f;
@@ -1266,6 +1272,15 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
     fetch_k(kb0, 0, 0);
     scores(0, 0, s0);
     fetch_k(kb0, 0, 1);
+    mask(s0, kb0 * KB, (uint32_t)now.z);
+    if (const float top = row_max(s0); top > -__builtin_inff()) {
+      l = 0.0f;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        neg[r] = MID - top;
+        s0[r] += MID - top;
+      }
+    }
     int sl = 0, vs = 0;  // slots of this block's keys and values
     for (int kb = kb0; kb < kb1; ++kb) {
       const int sl1 = sl == 2 ? 0 : sl + 1, sl2 = sl1 == 2 ? 0 : sl1 + 1;
@@ -1302,6 +1317,7 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
     }
   }
   if (wrow > last) return;
+  if (l == __builtin_inff()) l = 0.0f;
   l += __shfl_xor(l, 32);
   zsum += __shfl_xor(zsum, 32);
 #pragma unroll
