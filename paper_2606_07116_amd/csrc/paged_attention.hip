@@ -613,7 +613,9 @@ kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, 
 //   moves references (in fp16, offsets of 300 and 3000 steps left noise of 1.3 and 12 % of their
 //   norm in the other channels of values that are rotated back);
 // * the keys' zero-point term -z_j sum q, which can be far larger than the score, is a k-step of
-//   its own: A z_j and sum q as three fp16 pieces each, their six leading products;
+//   its own: A z_j and sum q as three fp16 pieces each, their six leading products.  Half of its 16
+//   products have z 2^12 times larger and the sum as much smaller, where the sum never leaves fp16's
+//   range; the other half have what A z_j leaves beyond the range there, of the largest keys;
 // * the score product starts from -m, the row's reference, so what it leaves are the exponents of
 //   the weights: per weight one exp2, half a conversion to fp16 and half a dot product for the
 //   sum.  A row takes its reference from the scores of the first tile that it sees, wherever they
@@ -651,7 +653,8 @@ struct alignas(16) Stage {
   uint8_t k[3][KB * (2 * D + 16)];  // per position: A c 2^-9, 8 fp16 per code word, in operand order
   uint8_t v[2][D * VROW];           // per channel (nibble * D / 8 + word): A (c - z) 2^-9 of the 64 positions
   struct Par {                      // what a block's codes are staged with
-    uint4 z[KB];                    // per position: the pieces of the keys' A z 2^-13
+    uint4 z[2][KB];                 // per position: the pieces of the keys' A z: [1] of A z / 2 up
+                                    // to 2^15, [0] of the rest / 2^13
     uint32_t a[KB];                 // the keys' A and A / 16
     uint32_t ab[KB];                // the values' A and -A z' 2^-9
     float rest[KB];                 // the values' A (z - z') 2^-9
@@ -927,12 +930,15 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
     if (!ok) p = make_uint2(0, 0);
     const float sk = fp16_bits_to_f32((uint16_t)p.x), zk = (float)(int16_t)(p.x >> 16);
     const float sv = fp16_bits_to_f32((uint16_t)p.y), zv = (float)(int16_t)(p.y >> 16);
-    // keys: A (8192 + |z|) stays below 2^28: A below 2^15, the pieces of A z 2^-13 as well
+    // keys: A (8192 + |z|) stays below 2^28: A below 2^15, the pieces of A z 2^-13 as well.  (No
+    // further below it than that takes: the other keys' bits go first.)
     const float kt = wave_max(sk * (8192.0f + fabsf(zk)));
-    if (__builtin_amdgcn_ldexpf(kt, -E) >= 0x1p28f) E = __builtin_amdgcn_frexp_expf(kt) - 25;
+    if (__builtin_amdgcn_ldexpf(kt, -E) >= 0x1p28f) E = __builtin_amdgcn_frexp_expf(kt) - 28;
     const float ka = __builtin_amdgcn_ldexpf(sk, -E);
-    const Pieces u = pieces(ka * zk * 0x1p-13f);
-    P.z[lane] = make_uint4(pk_f16(u.h1, u.h1), pk_f16(u.h2, u.h1), pk_f16(u.h2, u.h3), 0);
+    const float near = __builtin_amdgcn_fmed3f(ka * zk * 0.5f, -0x1p15f, 0x1p15f);
+    const Pieces u = pieces(near), v = pieces((ka * zk * 0.5f - near) * 0x1p-12f);
+    P.z[1][lane] = make_uint4(pk_f16(u.h1, u.h1), pk_f16(u.h2, u.h1), pk_f16(u.h2, u.h3), 0);
+    P.z[0][lane] = make_uint4(pk_f16(v.h1, v.h1), pk_f16(v.h2, v.h1), pk_f16(v.h2, v.h3), 0);
     P.a[lane] = pk_f16(ka, ka * 0.0625f);
     // values: A stays below 2^15
     const float vt = wave_max(sv);
@@ -987,6 +993,20 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
   // stand in such an order that half h of the lanes gets channels 16 h .. 16 h + 15 of the 32, two
   // code words; without a rotation the product is with 1.
   uint32_t qb[NS][4], zb[4] = {0, 0, 0, 0};
+  auto zero_terms = [&] {  // -16 sum q for this half of the zero-points' products
+    float sum = 0.0f;
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        sum = __builtin_amdgcn_fdot2(__builtin_bit_cast(h2_t, qb[s][k]),
+                                     h2_t{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
+    sum += __shfl_xor(sum, 32);
+    const Pieces v = pieces(h ? sum * -0x1p-8f : __builtin_amdgcn_fmed3f(-16.0f * sum, -65504.0f, 65504.0f));
+    zb[0] = pk_f16(v.h1, v.h2);
+    zb[1] = pk_f16(v.h1, v.h3);
+    zb[2] = pk_f16(v.h2, v.h1);
+  };
   int E;
   bool bad;  // the row is not finite: held at the end of fp16's range, it would give numbers
   {
@@ -1035,8 +1055,8 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
       sm2 *= hadamard_norm<D>();
     }
     // E: the largest query at 2^4, unless the first block's keys would leave their range.  Then
-    // queries beyond fp16's range stay at its end: scores over 2^25, where the others, in the same
-    // tile, keep their bits.
+    // queries beyond fp16's range, 2^12 above it, stay at its end: a channel of theirs makes over
+    // 2^21 of a score with one step of the largest key's codes.  The others keep their bits.
     float qm = 0.0f;
 #pragma unroll
     for (int i = 0; i < D / 2; ++i) qm = fmaxf(qm, fabsf(x[i >> 4][i & 15]));
@@ -1052,14 +1072,13 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
 #pragma unroll
     for (int k = 1; k < 8; ++k) qm = fmaxf(qm, s_qm[k]);
     E = uniform(-5 - max(__builtin_amdgcn_frexp_expf(qm), -100) - __builtin_amdgcn_frexp_expf(sm2));
-    if (kt > 0.0f) E = max(E, uniform(__builtin_amdgcn_frexp_expf(kt)) - 25);
+    if (kt > 0.0f) E = max(E, uniform(__builtin_amdgcn_frexp_expf(kt)) - 28);
     const float f = __builtin_amdgcn_ldexpf(sm2, E + 9);
     float check = 0.0f;
 #pragma unroll
     for (int i = 0; i < D / 2; ++i) check = __builtin_fmaf(x[i >> 4][i & 15], 0.0f, check);
     check += __shfl_xor(check, 32);
     bad = check != 0.0f;
-    float sum = 0.0f;
 #pragma unroll
     for (int s = 0; s < NS; ++s)
 #pragma unroll
@@ -1068,16 +1087,9 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
         h2_t p = {(_Float16)(f * x[s >> 1][8 * (s & 1) + k]),
                   (_Float16)(f * x[s >> 1][8 * (s & 1) + k + 4])};
         p = __builtin_elementwise_max(__builtin_elementwise_min(p, top), -top);
-        sum = __builtin_amdgcn_fdot2(p, h2_t{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
         qb[s][k] = __builtin_bit_cast(uint32_t, p);
       }
-    sum += __shfl_xor(sum, 32);
-    if (!h) {
-      const Pieces v = pieces(__builtin_amdgcn_fmed3f(-16.0f * sum, -65504.0f, 65504.0f));
-      zb[0] = pk_f16(v.h1, v.h2);
-      zb[1] = pk_f16(v.h1, v.h3);
-      zb[2] = pk_f16(v.h2, v.h1);
-    }
+    zero_terms();
   }
 
   f16_t o[ND];
@@ -1100,7 +1112,7 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
                                            16 * (k & 1));
   };
   auto fetch_k = [&](int kb, int slot, int tt) {
-    kz = S.par[kb & 3].z[32 * tt + ql];
+    kz = S.par[kb & 3].z[h][32 * tt + ql];
 #pragma unroll
     for (int k = 0; k < KA; ++k) kf[k] = key_at(slot, tt, k);
   };
@@ -1205,6 +1217,7 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
     }
   };
   auto rescale_q = [&](int to) {
+    if (Eq >= to) return;
     for (; Eq < to; Eq = min(Eq + 15, to)) {
       const _Float16 f = (_Float16)__builtin_amdgcn_ldexpf(1.0f, min(to - Eq, 15));
       auto grow = [&](uint32_t& x) {
@@ -1216,9 +1229,8 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
       for (int k = 0; k < NS; ++k)
 #pragma unroll
         for (int j = 0; j < 4; ++j) grow(qb[k][j]);
-#pragma unroll
-      for (int j = 0; j < 3; ++j) grow(zb[j]);
     }
+    zero_terms();
   };
 
   // Pipeline: while a tile's weights are formed, the next tile's scores are on the matrix cores;

@@ -135,3 +135,46 @@ def test_values_around_an_offset(offset, new, past, D):
     print(off / np.linalg.norm(ref[..., 1:]))
     assert off <= 1.5 * 2.0 ** -8 * np.linalg.norm(ref[..., 1:]) + 2.0 ** -22 * np.linalg.norm(ref[..., 0])
     assert np.linalg.norm((got - ref)[..., 0]) <= 2.0 ** -8 * np.linalg.norm(ref[..., 0])
+
+
+# ------------------------------------------------------------------ rows not seen
+def _last_position(key=None, value=None):
+    """Parameters of each sequence's last position: (scale, zero-point) of its key, of its value."""
+    def spoil(call):
+        for b, n in enumerate(call.lens):
+            page, at = call.slot(b, n - 1)
+            for j, what in ((0, key), (2, value)):
+                if what:
+                    call.host[2][page, :, at, j] = np.float16(what[0]).view(np.int16)
+                    call.host[2][page, :, at, j + 1] = what[1]
+    return spoil
+
+
+def _earlier_rows(new, past, spoil, D, one_sign=False, k_had=True):
+    """The error of the rows that do not see their sequence's last position, with it spoilt."""
+    def positive(q):
+        q[...] = np.abs(q)
+
+    call = Call(new, past, D=D, seed=sum(new) + D, queries=positive if one_sign else None)
+    ref = call.exact(1 / math.sqrt(D), k_had)
+    spoil(call)
+    got = call.run(1 / math.sqrt(D), k_had)
+    early = np.ones(len(ref), bool)
+    early[call.starts[1:] - 1] = False
+    e = _error(got[early], ref[early])
+    print(e)
+    return e
+
+
+@pytest.mark.parametrize("scale,zero", [(65504, 0), (65504, 15), (65504, 32767), (65504, -32768),
+                                        (300, 5), (300, 32767)])
+@pytest.mark.parametrize("one_sign", [False, True])
+@pytest.mark.parametrize("new,past", [([100], [0]), ([70, 3], [1500, 300]), ([4], [300])])
+@pytest.mark.parametrize("D", [64, 128])
+def test_huge_rows_behind(scale, zero, one_sign, new, past, D):
+    """A last token whose key and value have the largest scale that the quantizer writes (what an
+    overflow before it leaves) and the rows before it, which do not see it.  Their scaled codes may
+    become fp16 subnormals, 2^-8 of a step each: 2^-8 / sqrt(3) sm sk |q|, 0.001, in a score; with
+    half a bf16 step and the other roundings 2^-8 of the outputs' norm holds."""
+    assert _earlier_rows(new, past, _last_position((scale, zero), (scale, zero)), D, one_sign,
+                         k_had=not one_sign) <= 2.0 ** -8
