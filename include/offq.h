@@ -515,7 +515,8 @@ offq_status_t offq_kv_dequantize_paged(const uint8_t* k_codes, const uint8_t* v_
  *              first max_new are left as they were).
  *   page_table int32 [B, max_pages] (device): a sequence's pages in order.  A
  *              position whose page is outside [0, num_pages), or past the table,
- *              is not seen; a row that sees no position gives 0.
+ *              is not seen; a row that sees no position gives 0, one that sees a
+ *              position with a scale that is NaN or infinite gives NaN.
  *   out        bf16 [M, Hq D], row stride ldo (a multiple of 8), 16-byte aligned;
  *              it may not overlap q.
  *   workspace  caller-owned device buffer of at least

@@ -30,6 +30,14 @@ constexpr float LOWEST = -1e30f;  // a reference maximum below every score
 // (a uniform value that went through the vector units, a division for instance)
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
+// A position whose scales are not both finite (a row that was never written): its key's becomes
+// NaN, and so what sees it; its value's 0, since a weight of 0 times NaN or infinity would reach
+// the rows that do not.
+__device__ __forceinline__ uint2 for_those_who_see(uint2 par) {
+  const bool bad = ((par.x & 0x7C00u) == 0x7C00u) | ((par.y & 0x7C00u) == 0x7C00u);
+  return make_uint2(bad ? 0x7E00u : par.x, bad ? 0u : par.y);
+}
+
 // What a sequence asks for, lengths made safe whatever the tables hold: `rows` query rows
 // (token, head of the group) of a key/value head, the first of them token q0 at position pos0,
 // and `keys` positions that the last of them sees.
@@ -373,10 +381,11 @@ kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, 
     // (no branch here: behind one, the wait for the parameters takes in the next block's loads)
     const bool valid = (lane < 32) & ((x.ok >> (lane >> 4 & 1)) & 1) & (key < k_stop);
     const uint32_t vm = (uint32_t)__builtin_amdgcn_ballot_w64(valid);
-    const float sk = valid ? fp16_bits_to_f32((uint16_t)x.par.x) : 0.0f;
-    const float zk = valid ? (float)(int16_t)(x.par.x >> 16) : 0.0f;
-    const float sv = valid ? fp16_bits_to_f32((uint16_t)x.par.y) : 0.0f;
-    const float zv = valid ? (float)(int16_t)(x.par.y >> 16) : 0.0f;
+    const uint2 par = for_those_who_see(x.par);
+    const float sk = valid ? fp16_bits_to_f32((uint16_t)par.x) : 0.0f;
+    const float zk = valid ? (float)(int16_t)(par.x >> 16) : 0.0f;
+    const float sv = valid ? fp16_bits_to_f32((uint16_t)par.y) : 0.0f;
+    const float zv = valid ? (float)(int16_t)(par.y >> 16) : 0.0f;
     if (__builtin_amdgcn_ballot_w64(sv > v_lim)) {
       const float top = wave_max(sv);
       const float lim = __builtin_amdgcn_ldexpf(1.0f, __builtin_amdgcn_frexp_expf(top));
@@ -927,6 +936,7 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
   auto prepare = [&](int kb, int page, uint2 p, int E, int F) {
     typename Stage<D>::Par& P = S.par[kb & 3];
     const bool ok = ((uint32_t)page < (uint32_t)c.pages) & (kb * KB + lane < keys);
+    p = for_those_who_see(p);
     if (!ok) p = make_uint2(0, 0);
     const float sk = fp16_bits_to_f32((uint16_t)p.x), zk = (float)(int16_t)(p.x >> 16);
     const float sv = fp16_bits_to_f32((uint16_t)p.y), zv = (float)(int16_t)(p.y >> 16);
@@ -1061,10 +1071,11 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
 #pragma unroll
     for (int i = 0; i < D / 2; ++i) qm = fmaxf(qm, fabsf(x[i >> 4][i & 15]));
     qm = wave_max(qm);
+    const uint32_t kpar = for_those_who_see(fpar[0]).x;
     const float kt = wave_max(any && (uint32_t)fpage[0] < (uint32_t)c.pages &&
                                       kb0 * KB + lane < keys
-                                  ? fp16_bits_to_f32((uint16_t)fpar[0].x) *
-                                        (8192.0f + fabsf((float)(int16_t)(fpar[0].x >> 16)))
+                                  ? fp16_bits_to_f32((uint16_t)kpar) *
+                                        (8192.0f + fabsf((float)(int16_t)(kpar >> 16)))
                                   : 0.0f);
     if (lane == 0) s_qm[wave] = qm;
     __syncthreads();

@@ -151,7 +151,8 @@ def _last_position(key=None, value=None):
 
 
 def _earlier_rows(new, past, spoil, D, one_sign=False, k_had=True):
-    """The error of the rows that do not see their sequence's last position, with it spoilt."""
+    """The error of the rows that do not see their sequence's last position, with it spoilt, and the
+    rows that do."""
     def positive(q):
         q[...] = np.abs(q)
 
@@ -163,7 +164,7 @@ def _earlier_rows(new, past, spoil, D, one_sign=False, k_had=True):
     early[call.starts[1:] - 1] = False
     e = _error(got[early], ref[early])
     print(e)
-    return e
+    return e, got[~early]
 
 
 @pytest.mark.parametrize("scale,zero", [(65504, 0), (65504, 15), (65504, 32767), (65504, -32768),
@@ -177,4 +178,17 @@ def test_huge_rows_behind(scale, zero, one_sign, new, past, D):
     become fp16 subnormals, 2^-8 of a step each: 2^-8 / sqrt(3) sm sk |q|, 0.001, in a score; with
     half a bf16 step and the other roundings 2^-8 of the outputs' norm holds."""
     assert _earlier_rows(new, past, _last_position((scale, zero), (scale, zero)), D, one_sign,
-                         k_had=not one_sign) <= 2.0 ** -8
+                         k_had=not one_sign)[0] <= 2.0 ** -8
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("side", ["key", "value", "both"])
+@pytest.mark.parametrize("new,past", [([100], [0]), ([300], [30]), ([70, 3], [1500, 300]), ([4], [300])])
+@pytest.mark.parametrize("D", [64, 128])
+def test_rows_that_are_no_numbers_behind(value, side, new, past, D):
+    """Parameters that are no numbers at the last position (a page that was never written) touch
+    the one row that sees it and no other; that row is not a number."""
+    p = (value, 7)
+    spoil = _last_position(p if side != "value" else None, p if side != "key" else None)
+    error, last = _earlier_rows(new, past, spoil, D)
+    assert error <= 2.0 ** -8 and np.isnan(last).all()
