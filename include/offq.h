@@ -428,7 +428,7 @@ offq_status_t offq_kv_attention_prefill(const uint16_t* q, int64_t B, int64_t T,
  *                     and zero-point
  * with D = head_dim 64 or 128 and page_size a power of two, 16 .. 4096.
  * Position p of a sequence whose pages are t[0], t[1], ... is the slot
- * t[p / page_size] * page_size + p % page_size.
+ * t[p / page_size] * page_size + p % page_size.  M rows of a stride ld: M ld <= 2^40.
  * ------------------------------------------------------------------------- */
 
 /*

@@ -460,6 +460,10 @@ offq_status_t check_paged_pointers(const uint8_t* k_codes, const uint8_t* v_code
   return OFFQ_OK;
 }
 
+// M rows `ld` elements apart end past 2^40 elements, more than any memory (and, counted in bytes
+// below, far from 2^63)
+bool too_long(int64_t M, int64_t ld) { return M > 0 && ld > (int64_t(1) << 40) / M; }
+
 // [a, a + na) and [b, b + nb) share a byte
 bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
   const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
@@ -502,7 +506,7 @@ offq_status_t offq_rope_kv_paged(const uint16_t* qkv, int64_t ldq, int64_t M, in
   if (offq_status_t st = check_paged(Hkv, head_dim, num_pages, page_size, k_hadamard, v_hadamard))
     return st;
   // (a launch has less than 2^32 threads: a wave per token, head_dim / 8 lanes per row read back)
-  if (Hq > (1 << 16) || M > (1 << 26) - 4 || ldq > (int64_t(1) << 40) || ldo > (int64_t(1) << 40))
+  if (Hq > (1 << 16) || M > (1 << 26) - 4 || too_long(M, ldq) || too_long(M, ldo))
     return fail(OFFQ_ERR_UNSUPPORTED, "sizes too large");
   if (ldq < (Hq + 2 * Hkv) * head_dim || ldq % 8 || ldo < Hq * head_dim || ldo % 8)
     return fail(OFFQ_ERR_INVALID,
@@ -543,8 +547,8 @@ offq_status_t offq_kv_dequantize_paged(const uint8_t* k_codes, const uint8_t* v_
   if (M < 0) return fail(OFFQ_ERR_INVALID, "need M >= 0");
   if (offq_status_t st = check_paged(Hkv, head_dim, num_pages, page_size, k_hadamard, v_hadamard))
     return st;
-  if (M >= (1 << 28) || M * Hkv * head_dim >= (int64_t(1) << 35) - 4096 || ldk > (int64_t(1) << 40) ||
-      ldv > (int64_t(1) << 40))
+  if (M >= (1 << 28) || M * Hkv * head_dim >= (int64_t(1) << 35) - 4096 || (k_out && too_long(M, ldk)) ||
+      (v_out && too_long(M, ldv)))
     return fail(OFFQ_ERR_UNSUPPORTED, "sizes too large");
   if ((k_out && (ldk < Hkv * head_dim || ldk % 8)) || (v_out && (ldv < Hkv * head_dim || ldv % 8)))
     return fail(OFFQ_ERR_INVALID, "need ldk, ldv >= Hkv head_dim, multiples of 8");
@@ -608,7 +612,7 @@ offq_status_t offq_kv_attention_paged(const uint16_t* q, int64_t ldq, int64_t M,
   if (!paged_attention_sizes(M, B, Hq, Hkv, head_dim, max_new) ||
       max_pages > (int64_t(1) << 30) / page_size ||
       B * Hkv * (max_pages * page_size / 128 + 1) >= (int64_t(1) << 31) || num_pages > (int64_t(1) << 31) - 1 ||
-      ldq > (int64_t(1) << 40) || ldo > (int64_t(1) << 40))
+      too_long(M, ldq) || too_long(M, ldo))
     return fail(OFFQ_ERR_UNSUPPORTED, "sizes too large");
   if (M == 0 || B == 0 || max_new == 0) return ok();  // empty: pointers may be NULL
   if (!q || !q_starts || !seq_lens || !page_table || !out)
