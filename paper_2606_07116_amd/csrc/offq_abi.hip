@@ -469,6 +469,16 @@ bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
   const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
   return x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
 }
+
+// M rows of na elements at a and of nb at b share one.  (Rows of one stride may lie between each
+// other, as two parts of a wider row do.)
+bool rows_overlap(const uint16_t* a, int64_t lda, int64_t na, const uint16_t* b, int64_t ldb, int64_t nb,
+                  int64_t M) {
+  if (!overlap(a, 2 * ((M - 1) * lda + na), b, 2 * ((M - 1) * ldb + nb))) return false;
+  if (lda != ldb) return true;
+  const int64_t d = ((intptr_t)b - (intptr_t)a) / 2 % lda, at = d < 0 ? d + lda : d;
+  return at < na || at + nb > lda;
+}
 }  // namespace
 
 offq_status_t offq_rope_inv_freq(int32_t rotary_dim, double base, double factor, double low_turns,
@@ -526,8 +536,7 @@ offq_status_t offq_rope_kv_paged(const uint16_t* qkv, int64_t ldq, int64_t M, in
       !aligned(k_weight, 16) || !aligned(positions, 4) || !aligned(inv_freq, 4) ||
       !aligned(slots, 8))
     return fail(OFFQ_ERR_INVALID, "misaligned pointer (qkv, q_out, weights: 16 B; slots: 8 B)");
-  if (overlap(qkv, 2 * ((M - 1) * ldq + (Hq + 2 * Hkv) * head_dim), q_out,
-              2 * ((M - 1) * ldo + Hq * head_dim)))
+  if (rows_overlap(qkv, ldq, (Hq + 2 * Hkv) * head_dim, q_out, ldo, Hq * head_dim, M))
     return fail(OFFQ_ERR_INVALID, "q_out overlaps qkv");
   if (offq_status_t st = check_device()) return st;
   const offq::PagedCache c = {k_codes, v_codes, kv_params, num_pages, ilog2_pow2(page_size),
@@ -557,13 +566,7 @@ offq_status_t offq_kv_dequantize_paged(const uint8_t* k_codes, const uint8_t* v_
   if (offq_status_t st = check_paged_pointers(k_codes, v_codes, kv_params)) return st;
   if (!aligned(slots, 8) || !aligned(k_out, 16) || !aligned(v_out, 16))
     return fail(OFFQ_ERR_INVALID, "misaligned pointer (k_out, v_out: 16 B; slots: 8 B)");
-  if (k_out && v_out &&
-      overlap(k_out, 2 * ((M - 1) * ldk + Hkv * head_dim), v_out,
-              2 * ((M - 1) * ldv + Hkv * head_dim)) &&
-      !(ldk == ldv && ldk >= 2 * Hkv * head_dim &&
-        (k_out + Hkv * head_dim <= v_out ? v_out + Hkv * head_dim <= k_out + ldk
-                                         : v_out + Hkv * head_dim <= k_out &&
-                                               k_out + Hkv * head_dim <= v_out + ldv)))
+  if (k_out && v_out && rows_overlap(k_out, ldk, Hkv * head_dim, v_out, ldv, Hkv * head_dim, M))
     return fail(OFFQ_ERR_INVALID, "k_out overlaps v_out");
   if (offq_status_t st = check_device()) return st;
   // the kernel only reads the cache
@@ -625,7 +628,7 @@ offq_status_t offq_kv_attention_paged(const uint16_t* q, int64_t ldq, int64_t M,
   if (need > 0 && (!workspace || workspace_bytes < need))
     return fail(OFFQ_ERR_INVALID, "workspace of %lld bytes, need %lld",
                 (long long)(workspace ? workspace_bytes : 0), (long long)need);
-  if (overlap(q, 2 * ((M - 1) * ldq + Hq * head_dim), out, 2 * ((M - 1) * ldo + Hq * head_dim)))
+  if (rows_overlap(q, ldq, Hq * head_dim, out, ldo, Hq * head_dim, M))
     return fail(OFFQ_ERR_INVALID, "out overlaps q");
   if (offq_status_t st = check_device()) return st;
   const offq::PagedCache c = {const_cast<uint8_t*>(k_codes), const_cast<uint8_t*>(v_codes),
