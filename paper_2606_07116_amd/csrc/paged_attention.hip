@@ -816,6 +816,7 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
   constexpr int NV = D / 8;    // code words of a row
   __shared__ Stage<D> S;
   __shared__ float s_qm[8];
+  __shared__ int2 s_qe[8];
   const int tid = (int)__builtin_amdgcn_workitem_id_x();
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int ql = lane & 31, h = lane >> 5;
@@ -1064,12 +1065,20 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
           }
       sm2 *= hadamard_norm<D>();
     }
-    // E: the largest query at 2^4, unless the first block's keys would leave their range.  Then
-    // queries beyond fp16's range, 2^12 above it, stay at its end: a channel of theirs makes over
-    // 2^21 of a score with one step of the largest key's codes.  The others keep their bits.
+    // E: the largest query at 2^4, but the rows' mean (of their largest ones' exponents) no lower than
+    // 2^-4, so that a row of garbage leaves the others their bits, and no less than the first block's
+    // keys take.  A row that is too large for that, 2^19 above the mean, is made smaller as a whole:
+    // its scores are over 2^16 all the same, unless the keys are tiny to the others.  Queries that
+    // later keys raise beyond fp16's range, by 2^12 and more, stay at its end: a channel of theirs
+    // makes over 2^21 of a score with one step of the largest key's codes.
     float qm = 0.0f;
 #pragma unroll
     for (int i = 0; i < D / 2; ++i) qm = fmaxf(qm, fabsf(x[i >> 4][i & 15]));
+    qm = fmaxf(qm, __shfl_xor(qm, 32));
+    if (!(qm < __builtin_inff())) qm = 0.0f;
+    const int qe = max(__builtin_amdgcn_frexp_expf(qm), -100);  // this row's
+    const bool counts = qm > 0.0f && !h;
+    const int2 qes = make_int2(wave_add(counts ? qe : 0), wave_add(counts));
     qm = wave_max(qm);
     const uint32_t kpar = for_those_who_see(fpar[0]).x;
     const float kt = wave_max(any && (uint32_t)fpage[0] < (uint32_t)c.pages &&
@@ -1077,14 +1086,23 @@ __global__ __launch_bounds__(512, 1) void kv_attention_paged_tile_kernel(
                                   ? fp16_bits_to_f32((uint16_t)kpar) *
                                         (8192.0f + fabsf((float)(int16_t)(kpar >> 16)))
                                   : 0.0f);
-    if (lane == 0) s_qm[wave] = qm;
+    if (lane == 0) {
+      s_qm[wave] = qm;
+      s_qe[wave] = qes;
+    }
     __syncthreads();
-    qm = s_qm[0];
+    int2 sum = make_int2(0, 0);
 #pragma unroll
-    for (int k = 1; k < 8; ++k) qm = fmaxf(qm, s_qm[k]);
-    E = uniform(-5 - max(__builtin_amdgcn_frexp_expf(qm), -100) - __builtin_amdgcn_frexp_expf(sm2));
+    for (int k = 0; k < 8; ++k) {
+      qm = fmaxf(qm, s_qm[k]);
+      sum = make_int2(sum.x + s_qe[k].x, sum.y + s_qe[k].y);
+    }
+    const int mean = (int)__builtin_floorf((float)sum.x / (float)max(sum.y, 1));
+    E = uniform(max(-5 - max(__builtin_amdgcn_frexp_expf(qm), -100), sum.y ? -13 - mean : -1000) -
+                __builtin_amdgcn_frexp_expf(sm2));
     if (kt > 0.0f) E = max(E, uniform(__builtin_amdgcn_frexp_expf(kt)) - 28);
-    const float f = __builtin_amdgcn_ldexpf(sm2, E + 9);
+    float f = __builtin_amdgcn_ldexpf(sm2, E + 9);
+    f = __builtin_amdgcn_ldexpf(f, min(0, 15 - qe - __builtin_amdgcn_frexp_expf(f)));
     float check = 0.0f;
 #pragma unroll
     for (int i = 0; i < D / 2; ++i) check = __builtin_fmaf(x[i >> 4][i & 15], 0.0f, check);

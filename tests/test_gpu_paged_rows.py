@@ -192,3 +192,29 @@ def test_rows_that_are_no_numbers_behind(value, side, new, past, D):
     spoil = _last_position(p if side != "value" else None, p if side != "key" else None)
     error, last = _earlier_rows(new, past, spoil, D)
     assert error <= 2.0 ** -8 and np.isnan(last).all()
+
+
+@pytest.mark.parametrize("value", [3e4, 1e10, 1e30, 3e38])
+@pytest.mark.parametrize("first", ["absent", "zero", "tiny", "as the others"])
+@pytest.mark.parametrize("new,past", [([90], [200]), ([70, 3], [1500, 300]), ([5], [300])])
+def test_huge_queries_beside(value, first, new, past):
+    """One element of one query is huge and the first positions (64 and more) have no pages, no
+    scale, or scales of 2^-24: the other rows stay as exact as they are (2^-8 of the outputs' norm)
+    when later keys bring the scores of their size."""
+    def start(call):
+        for b in range(len(new)):
+            for i in range(5):
+                if first == "absent":
+                    call.table[b, i] = -1
+                elif first != "as the others":
+                    call.host[2][call.table[b, i], ..., ::2] = first == "tiny"
+
+    call = Call(new, past, seed=sum(new), cache=start)
+    ref = call.exact(1 / math.sqrt(128))
+    call.q[4, 1, 7] = value
+    got = call.run(1 / math.sqrt(128))
+    others = np.ones(ref.shape[:2], bool)
+    others[4, 1] = False
+    e = _error(got[others], ref[others])
+    print(e)
+    assert e <= 2.0 ** -8
