@@ -425,7 +425,7 @@ offq_status_t offq_kv_attention_prefill(const uint16_t* q, int64_t B, int64_t T,
  *   k_codes, v_codes  uint8 [num_pages, Hkv, page_size, D/2], 16-byte aligned
  *   kv_params         int16 [num_pages, Hkv, page_size, 4], 8-byte aligned: the
  *                     key's scale (fp16 bits) and zero-point, the value's scale
- *                     and zero-point
+ *                     and zero-point (scales as the quantizer writes them, or 0)
  * with D = head_dim 64 or 128 and page_size a power of two, 16 .. 4096.
  * Position p of a sequence whose pages are t[0], t[1], ... is the slot
  * t[p / page_size] * page_size + p % page_size.  M rows of a stride ld: M ld <= 2^40.

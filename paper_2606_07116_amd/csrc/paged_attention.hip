@@ -74,7 +74,7 @@ __device__ __forceinline__ Seq sequence(const PagedAttentionArgs& a, int log2p, 
 // The zero-point terms are kept out of the products (sum q, sum w z in fp32), so large offsets
 // cost no accuracy.  The query and the weights p sv are rounded to fp16 (2^-11), scaled so that
 // neither tiny nor huge scales leave its range: the query by a power of two of its row, the
-// weights by one that follows the largest value scale met.
+// weights by one that follows the largest value scale met (values of scales 2^21 below it lose bits).
 //
 // Measured (a large copy here: 4.9 TB/s, reads alone 6.2): 8 x 32768 positions of 32 heads of their
 // own 205 us, 5.6 TB/s; 24 ragged sequences of up to 30000, five query heads to each of 8, 70 us
@@ -643,9 +643,10 @@ kv_attention_paged_few_kernel(PagedAttentionArgs a, PagedCache c, int few_rows, 
 // over workgroups and the rows joined by a second kernel.
 //
 // Measured: 2.2 us per tile and block, 920 TFLOP/s inside, where a large library product reaches
-// 1150; three prompts of up to 8000 tokens 655 us with the tiles' 8 us each besides their blocks.
+// 1150; three prompts of up to 8000 tokens 648 to 683 us (by the card's clock) with the tiles' 8 us
+// each besides their blocks, 7 % more where the values' zero-points lie beyond their codes.
 // What bounds it are a block's phases, which two waves per SIMD do not hide from each other: matrix
-// cores busy 44 % of the time, vector units 44 %, LDS 35 %.  Not faster: 64 rows a wave and one
+// cores busy 44 % of the time, vector units 43 %, LDS 35 %.  Not faster: 64 rows a wave and one
 // wave per SIMD (twice the time: accumulators moved about), the keys' zero-points in their codes
 // and no k-step for them (2 %, and a branch for far ones takes that back), half a block between
 // the waves of a SIMD, priorities, scheduling groups, two chains of accumulators.
@@ -1551,7 +1552,10 @@ Shape attention_shape(int64_t M, int64_t B, int64_t Hq, int64_t Hkv, int D, int6
   // but its time grows with the row tiles, and at 64 rows of 128 channels it runs out of
   // registers: 8 new tokens of 8 heads, 4 x 5000 positions: 92 us there, 36 us as a tile that is
   // three quarters empty; 5 tokens 36 us there, 38 as a tile, with 64 x 5000 241 and 334.  64 rows
-  // of 64 channels: 32 us there, 51 us as a tile.
+  // of 64 channels: 32 us there, 51 us as a tile.  Beside sequences of many rows it takes 16, and
+  // those between go to tiles: with three row tiles every one of its workgroups would have their
+  // registers (128 channels, beside a prompt of 1000: 32 single tokens of 4 heads after 5000 90 us,
+  // with 48 rows 169; 32 x 5 tokens of 8 heads 166 and 187; 4 x 5 tokens 104 and 99).
   f.many = most > (D == 128 ? 48 : 64);
   f.few = !f.many || B > 1;  // a single sequence of many rows: one launch
   f.row_tiles = f.many || most <= 16 ? 1 : most <= 32 ? 2 : most <= 48 ? 3 : 4;
