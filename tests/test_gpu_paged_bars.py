@@ -41,8 +41,8 @@ def test_shapes(i):
     _check(new, past, Hq, Hkv, D, v_had, seed=i)
 
 
-# rows of a key/value head that no call had so far: three row tiles at 128 channels, three and four
-# at 64, as one chunk (up to 512 positions of the page table) and as joined ones; without a rotation
+# the few-row kernel with three row tiles at 128 channels, three and four at 64, as one chunk (up to
+# 512 positions of the page table) and as joined ones
 @pytest.mark.parametrize("rows,D", [(33, 128), (40, 128), (48, 128), (40, 64), (48, 64), (49, 64), (64, 64)])
 @pytest.mark.parametrize("past", [0, 77, 400, 1500])
 @pytest.mark.parametrize("k_had,v_had", [(True, False), (False, True)])
